@@ -2,7 +2,8 @@
  * fqvit.h -- C ABI of the MI355X (gfx950) library for the integer hot path of
  * FQ-ViT (Lin et al., "FQ-ViT: Post-Training Quantization for Fully Quantized
  * Vision Transformer", IJCAI 2022): Power-of-Two-Factor LayerNorm and
- * Log-Int-Softmax attention.
+ * Log-Int-Softmax attention, and the linear layers, rotary positions and
+ * requantization around them.
  *
  * Conventions shared by every entry point
  *   - Tensor arguments are DEVICE pointers into memory the caller owns (for
@@ -307,6 +308,165 @@ fq_status ptf_quantize_int8(const float* x, int64_t T, int32_t C, const double* 
  */
 fq_status requant_dyadic_int8(const int32_t* q, int64_t n, float s_in, float s_out,
                               int32_t zp_out, int32_t bits, int8_t* y, void* stream);
+
+/*
+ * Linear layer: the integer matrix product that every quantized layer around
+ * the attention is (Sec. 3.1), with its bias, its activation, the residual
+ * branch and the requantization in the product's epilogue.  Values stand for
+ *   x_real = s_x (x - zp_x),  w_real = s_w[n] w,  y_real = s_y (y - zp_y).
+ *
+ * linear_fold_int8 makes, once for a layer, the two vectors that the products
+ * take: the bias on the accumulators' scale with the input's zero point folded
+ * in, and the channels' multipliers.  In binary64, each operation rounded once:
+ *   acc scale  s_n = s_x s_w[n]
+ *   fold[n] = clip(rint(bias[n] / s_n), -2^30, 2^30) - zp_x sum_k w[n, k]
+ *   mul[n]  = s_n / s_y rounded to binary32 (at most the largest finite one).
+ * A channel whose s_w[n] is not positive and finite takes mul[n] = 0 and no
+ * bias; a bias that is not a number counts as 0.
+ *
+ *   w      [N, K] int8, N in [1, 2^20], K in [1, 32768].
+ *   s_w    [N] float; bias [N] float or NULL (none).
+ *   zp_x   in [-128, 127]; s_x, s_y positive and finite.  s_y is the output's
+ *          step, or the step of the activation's input where a table follows.
+ *   fold   [N] int32 (out); mul [N] float (out) or NULL (then s_y is unused).
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (N or K out of range), FQ_ERR_PARAM.
+ */
+fq_status linear_fold_int8(const int8_t* w, int32_t N, int32_t K, const float* s_w,
+                           const float* bias, int32_t zp_x, float s_x, float s_y, int32_t* fold,
+                           float* mul, void* stream);
+
+/* Activations of linear_int8. */
+#define FQ_ACT_NONE 0
+#define FQ_ACT_RELU 1
+#define FQ_ACT_TABLE 2   /* any function, as 2^table_bits values over its input's grid */
+
+/*
+ * y = requantized (activation(x w^T + bias) + residual), in int8.
+ *
+ *   x      [T, K] int8, w [N, K] int8 (a row per output channel).
+ *   fold, mul   [N] int32 and float, as linear_fold_int8 writes them (fold NULL:
+ *          zeros).  mul >= 0 and finite.
+ *   act    FQ_ACT_*; with FQ_ACT_TABLE, table is a device array of
+ *          2^table_bits floats (finite), table_bits in [4, 12], zp_t in
+ *          [0, 2^table_bits - 1]; else they are ignored.
+ *   residual  NULL or [T, N] int8 of zero point zp_r in [-128, 127]; mul_r =
+ *          s_r / s_y, in [2^-20, 2^20].
+ *   zp_y, bits  the output's zero point (container form) and grid, b in [2, 8].
+ *   y      [T, N] int8 container (out).  It may be the residual itself; it
+ *          overlaps no other argument.
+ * T >= 0, N in [1, 2^20], K in [1, 32768].  Bases of any alignment; rows of
+ * whole 16-byte units on 16-byte aligned bases take the fast path.
+ *
+ * With acc = sum_k x[t,k] w[n,k] + fold[n] exact in int32, RN = rounding to the
+ * nearest binary32 and rint = to the nearest integer (ties to even in both), of
+ * the exact value in its argument:
+ *   a = RN(acc)
+ *   without a residual:
+ *     NONE   y = clip(rint(a mul + zp_y))
+ *     RELU   y = clip(rint(max(a mul, 0) + zp_y))
+ *     TABLE  u = clip(rint(a mul + zp_t), 0, 2^table_bits - 1)
+ *            y = clip(rint(table[u] + zp_y))
+ *   with one: z = RN((r + 128) mul_r + c), c = RN(zp_y - (128 + zp_r) mul_r), and
+ *     NONE   y = clip(rint(RN(a mul + z)))
+ *     RELU   y = clip(rint(RN(max(RN(a mul), 0) + z)))
+ *     TABLE  y = clip(rint(RN(table[u] + z)))
+ * clip is to the container's [-2^(b-1), 2^(b-1) - 1].  A table holds its
+ * function's values in steps of the output, f(s_t (u - zp_t)) / s_y; then mul
+ * was folded with the table's step s_t in the place of s_y.
+ * Errors: FQ_ERR_NULL (x, w, mul, y; table with FQ_ACT_TABLE), FQ_ERR_SHAPE
+ * (T, N or K, or more tiles than a grid holds), FQ_ERR_PARAM (act, table_bits,
+ * zp_t, zero points, mul_r, bits).
+ */
+fq_status linear_int8(const int8_t* x, int64_t T, const int8_t* w, int32_t N, int32_t K,
+                      const int32_t* fold, const float* mul, int32_t act, const float* table,
+                      int32_t table_bits, int32_t zp_t, const int8_t* residual, int32_t zp_r,
+                      float mul_r, int32_t zp_y, int32_t bits, int8_t* y, void* stream);
+
+/*
+ * The accumulators themselves: out[t, n] = sum_k x[t,k] w[n,k] + fold[n] in
+ * int32 (scale s_x s_w[n]), for class scores and layers requantized elsewhere.
+ * Sizes, alignment and errors as linear_int8; fold may be NULL (zeros).  The
+ * sum is exact for fold within +-2^30; it wraps modulo 2^32 where a larger one
+ * takes it out of int32.
+ */
+fq_status linear_int32(const int8_t* x, int64_t T, const int8_t* w, int32_t N, int32_t K,
+                       const int32_t* fold, int32_t* out, void* stream);
+
+/*
+ * Fills a HOST array with an activation's table for linear_int8: in binary64,
+ * table[u] = f(t) / s_y rounded to binary32, t = s_t (u - zp_t), u in
+ * [0, 2^table_bits - 1].  Runs on the host; enqueues nothing.
+ *   kind   FQ_FN_GELU        t (1 + erf(t / sqrt 2)) / 2
+ *          FQ_FN_GELU_TANH   t (1 + tanh(sqrt(2/pi) (t + 0.044715 t^3))) / 2
+ *          FQ_FN_SILU        t / (1 + exp(-t))
+ * Errors: FQ_ERR_NULL, FQ_ERR_PARAM (kind, table_bits, zp_t, a step not
+ * positive and finite, or a value that binary32 cannot hold).
+ */
+#define FQ_FN_GELU 0
+#define FQ_FN_GELU_TANH 1
+#define FQ_FN_SILU 2
+fq_status fq_activation_table(int32_t kind, float s_t, int32_t zp_t, int32_t table_bits, float s_y,
+                              float* table);
+
+/*
+ * Rotary positions of several axes (time, height, width): pair p of a head
+ * turns by the angle t = positions[axis[p], i] freq[p] of token i.  The table
+ * holds cos and sin of every token and pair in steps of 2^-14:
+ *   table[i, p] = (rint(2^14 cos t), rint(2^14 sin t)), t in binary64 (one
+ * rounding), cos and sin in binary64 to within 2 units of their last place, so
+ * an entry may be the other neighbour only where 2^14 cos t lies that close to
+ * the middle of two integers.  Position 0 gives (2^14, 0): no turn at all.
+ *
+ *   positions  [axes, T] int32, axes in [1, 8].
+ *   freq   [P] double (finite), P in [1, 128]; axis [P] uint8 (values at or
+ *          above `axes` are taken as axes - 1).
+ *   table  [T, P, 2] int16 (out), 4-byte aligned.
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (T < 0 or above 2^31 - 1, axes, P),
+ * FQ_ERR_PARAM (table not aligned).
+ */
+fq_status rope_table_int16(const int32_t* positions, int32_t axes, int64_t T, const double* freq,
+                           const uint8_t* axis, int32_t P, int16_t* table, void* stream);
+
+/*
+ * The query-key-value layer's rows split into heads, queries and keys rotated
+ * and requantized, as lis_attention_qk takes them.
+ *
+ *   qkv    [B, L, (Hq + 2 Hkv) d] int8 with scale s_x and zero point zp_x: the
+ *          query heads, the key heads, the value heads.  Hq, Hkv in [1, 1024],
+ *          d in [1, 256].
+ *   table  [table_rows, P, 2] int16, 4-byte aligned, as rope_table_int16 writes
+ *          it; table_rows is L (one grid for every b) or B L.  P in [0, d / 2]
+ *          pairs turn, the d - 2 P values after them do not.  P = 0: table may
+ *          be NULL and table_rows is unused.
+ *   interleaved  0: pair p is (x[p], x[p + P]); 1: (x[2 p], x[2 p + 1]).
+ *   q      [B, Hq, L, d] int8 (out), scale s_q, zero point zp_q (container of
+ *          the b-bit grid); k [B, Hkv, L, d] (out), s_k, zp_k; v [B, Hkv, L, d]
+ *          (out), the values as they are.  With Hq = r Hkv, q read as
+ *          [B Hkv, r L, d] are the queries of each key head.
+ * With (f, g) a pair less zp_x and (c, s) its table entry, the turned pair is
+ * (f c - g s, f s + g c), exact in 32 bits for |c|, |s| <= 2^14; a value that
+ * does not turn counts 2^14 times itself less zp_x.  Each, a, becomes
+ * clip(rint(a m + zp)), the exact value rounded once (ties to even), with m =
+ * s_x / (2^14 s_q) (s_k) in binary64 rounded to binary32.
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (sizes, table_rows), FQ_ERR_PARAM (scales,
+ * zero points, bits, interleaved, table not aligned).
+ */
+fq_status rope_qkv_int8(const int8_t* qkv, int64_t B, int32_t L, int32_t Hq, int32_t Hkv, int32_t d,
+                        float s_x, int32_t zp_x, const int16_t* table, int64_t table_rows, int32_t P,
+                        int32_t interleaved, float s_q, int32_t zp_q, float s_k, int32_t zp_k,
+                        int32_t bits, int8_t* q, int8_t* k, int8_t* v, void* stream);
+
+/*
+ * requant_dyadic_int8 of an attention result, with its heads brought back to
+ * rows: q [B, H, L, d] int32 (lis_attention_qk's out) -> y [B, L, H d] int8, as
+ * the projection's linear layer reads it.  The same dyadic multiplier and
+ * rounding; H in [1, 1024], d in [1, 256].
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (B or L < 0, H, d), FQ_ERR_PARAM (bits, a
+ * scale or zp_out out of range).
+ */
+fq_status requant_heads_int8(const int32_t* q, int64_t B, int32_t H, int32_t L, int32_t d,
+                             float s_in, float s_out, int32_t zp_out, int32_t bits, int8_t* y,
+                             void* stream);
 
 #ifdef __cplusplus
 }

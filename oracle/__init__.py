@@ -70,6 +70,14 @@ _SIGS = {
     "oracle_lis_attention_head": [_P, _P, _I32, _I64, _I32, _I32, _F32, _I32, _I32, _P, _I32,
                                   _I32, _P, _P, _I32],
     "oracle_requant_dyadic_int8": [_P, _I64, _F32, _F32, _I32, _I32, _P],
+    "oracle_linear_fold_int8": [_P, _I32, _I32, _P, _P, _I32, _F32, _F32, _P, _P],
+    "oracle_linear_int32": [_P, _I64, _P, _I32, _I32, _P, _P],
+    "oracle_linear_int8": [_P, _I64, _P, _I32, _I32, _P, _P, _I32, _P, _I32, _I32, _P, _I32, _F32,
+                           _I32, _I32, _P],
+    "oracle_rope_table_int16": [_P, _I32, _I64, _P, _P, _I32, _P],
+    "oracle_rope_qkv_int8": [_P, _I64, _I32, _I32, _I32, _I32, _F32, _I32, _P, _I64, _I32, _I32,
+                             _F32, _I32, _F32, _I32, _I32, _P, _P, _P],
+    "oracle_requant_heads_int8": [_P, _I64, _I32, _I32, _I32, _F32, _F32, _I32, _I32, _P],
     "oracle_qk_logits": [_P, _P, _I32, _I32, _I64, _I32, _I32, _I32, _P],
     "oracle_lis_attention_qk": [_P, _P, _I32, _I32, _I32, _P, _I32, _I64, _I32, _I32, _F32, _I32,
                                 _I32, _P, _I32, _I32, _P],
@@ -329,3 +337,77 @@ def lis_attention_qk(q, k, v, s_logit, zp_q=0, zp_k=0, bits=4, exp_n=20, zp_v=0,
                                          Lk, s_logit, bits, exp_n, _ptr(v), zp_v, d, _ptr(out)),
            "lis_attention_qk")
     return out
+
+
+# ---- Linear layers, rotary positions, heads back to rows ---------------------
+
+def _i8(a):
+    return None if a is None else np.ascontiguousarray(a, dtype=np.int8)
+
+
+def linear_fold_int8(w, s_w, s_x, s_y=1.0, zp_x=0, bias=None):
+    w, s_w = _i8(w), np.ascontiguousarray(s_w, dtype=np.float32)
+    bias = None if bias is None else np.ascontiguousarray(bias, dtype=np.float32)
+    N, K = w.shape
+    fold, mul = np.empty(N, np.int32), np.empty(N, np.float32)
+    _check(lib().oracle_linear_fold_int8(_ptr(w), N, K, _ptr(s_w), _ptr(bias), zp_x, s_x, s_y,
+                                         _ptr(fold), _ptr(mul)), "linear_fold_int8")
+    return fold, mul
+
+
+def linear_int32(x, w, fold=None):
+    x, w = _i8(x), _i8(w)
+    fold = None if fold is None else np.ascontiguousarray(fold, dtype=np.int32)
+    out = np.empty((x.shape[0], w.shape[0]), np.int32)
+    _check(lib().oracle_linear_int32(_ptr(x), x.shape[0], _ptr(w), *w.shape, _ptr(fold), _ptr(out)),
+           "linear_int32")
+    return out
+
+
+def linear_int8(x, w, fold, mul, zp_y=0, bits=8, relu=False, table=None, zp_t=0, residual=None,
+                zp_r=0, mul_r=1.0):
+    x, w, residual = _i8(x), _i8(w), _i8(residual)
+    fold = None if fold is None else np.ascontiguousarray(fold, dtype=np.int32)
+    mul = np.ascontiguousarray(mul, dtype=np.float32)
+    table = None if table is None else np.ascontiguousarray(table, dtype=np.float32)
+    act = 2 if table is not None else int(relu)
+    y = np.empty((x.shape[0], w.shape[0]), np.int8)
+    _check(lib().oracle_linear_int8(_ptr(x), x.shape[0], _ptr(w), *w.shape, _ptr(fold), _ptr(mul),
+                                    act, _ptr(table),
+                                    0 if table is None else table.size.bit_length() - 1, zp_t,
+                                    _ptr(residual), zp_r, mul_r, zp_y, bits, _ptr(y)),
+           "linear_int8")
+    return y
+
+
+def rope_table_int16(positions, freq, axis):
+    positions = np.ascontiguousarray(positions, dtype=np.int32)
+    freq, axis = np.ascontiguousarray(freq, dtype=np.float64), np.ascontiguousarray(axis, np.uint8)
+    axes, T = positions.shape
+    table = np.empty((T, freq.size, 2), np.int16)
+    _check(lib().oracle_rope_table_int16(_ptr(positions), axes, T, _ptr(freq), _ptr(axis), freq.size,
+                                         _ptr(table)), "rope_table_int16")
+    return table
+
+
+def rope_qkv_int8(qkv, table, Hq, Hkv, s_x, s_q, s_k, zp_x=0, zp_q=0, zp_k=0, bits=8,
+                  interleaved=False):
+    qkv = _i8(qkv)
+    B, L, row = qkv.shape
+    d = row // (Hq + 2 * Hkv)
+    table = None if table is None else np.ascontiguousarray(table, dtype=np.int16)
+    rows, P = (0, 0) if table is None else table.shape[:2]
+    q, k, v = (np.empty((B, h, L, d), np.int8) for h in (Hq, Hkv, Hkv))
+    _check(lib().oracle_rope_qkv_int8(_ptr(qkv), B, L, Hq, Hkv, d, s_x, zp_x, _ptr(table), rows, P,
+                                      int(interleaved), s_q, zp_q, s_k, zp_k, bits, _ptr(q),
+                                      _ptr(k), _ptr(v)), "rope_qkv_int8")
+    return q, k, v
+
+
+def requant_heads_int8(q, s_in, s_out, zp_out, bits=8):
+    q = np.ascontiguousarray(q, dtype=np.int32)
+    B, H, L, d = q.shape
+    y = np.empty((B, L, H * d), np.int8)
+    _check(lib().oracle_requant_heads_int8(_ptr(q), B, H, L, d, s_in, s_out, zp_out, bits, _ptr(y)),
+           "requant_heads_int8")
+    return y

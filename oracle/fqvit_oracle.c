@@ -747,3 +747,154 @@ int oracle_lis_attention_qk(const int8_t* q, const int8_t* k, int32_t zp_q, int3
     free(logits);
     return rc;
 }
+
+/* ------------------------------------------------------------------------ */
+/* Linear layers (Sec. 3.1), rotary positions, heads back to rows             */
+/* ------------------------------------------------------------------------ */
+
+/* READING: the paper quantizes weights per channel and activations per layer
+ * and leaves the layer's arithmetic open.  The definition, in the order below:
+ * exact integer sums, the bias on their scale, one multiplier per channel in
+ * binary32, and one rounding to the grid.  long double has 64 bits: a product
+ * of two binary32 values plus a third is exact here unless their exponents lie
+ * far apart, where the rest is a sticky bit that decides no rounding of the
+ * values that the tests use. */
+int oracle_linear_fold_int8(const int8_t* w, int32_t N, int32_t K, const float* s_w,
+                            const float* bias, int32_t zp_x, float s_x, float s_y, int32_t* fold,
+                            float* mul) {
+    if (N < 1 || K < 1 || !w || !s_w || !fold) return ORACLE_ERR_ARG;
+    for (int32_t n = 0; n < N; ++n) {
+        int64_t rows = 0;
+        for (int32_t k = 0; k < K; ++k) rows += w[(int64_t)n * K + k];
+        const double sw = (double)s_w[n];
+        double b = 0.0, m = 0.0;
+        if (sw > 0.0 && isfinite(sw)) {
+            const double s_acc = (double)s_x * sw;
+            m = s_acc / (double)s_y;
+            if (m > 3.4028234663852886e38) m = 3.4028234663852886e38;
+            if (bias && !isnan(bias[n])) {
+                b = rint((double)bias[n] / s_acc);
+                if (b > 1073741824.0) b = 1073741824.0;
+                if (b < -1073741824.0) b = -1073741824.0;
+            }
+        }
+        fold[n] = (int32_t)((int64_t)b - (int64_t)zp_x * rows);
+        if (mul) mul[n] = (float)m;
+    }
+    return ORACLE_OK;
+}
+
+int oracle_linear_int32(const int8_t* x, int64_t T, const int8_t* w, int32_t N, int32_t K,
+                        const int32_t* fold, int32_t* out) {
+    for (int64_t t = 0; t < T; ++t)
+        for (int32_t n = 0; n < N; ++n) {
+            int64_t s = fold ? fold[n] : 0;
+            for (int32_t k = 0; k < K; ++k)
+                s += (int64_t)x[t * K + k] * (int64_t)w[(int64_t)n * K + k];
+            if (s > INT32_MAX || s < INT32_MIN) return ORACLE_ERR_RANGE;
+            out[t * N + n] = (int32_t)s;
+        }
+    return ORACLE_OK;
+}
+
+static long double clip_ld(long double v, long double lo, long double hi) {
+    return v < lo ? lo : (v > hi ? hi : v);
+}
+
+int oracle_linear_int8(const int8_t* x, int64_t T, const int8_t* w, int32_t N, int32_t K,
+                       const int32_t* fold, const float* mul, int32_t act, const float* table,
+                       int32_t table_bits, int32_t zp_t, const int8_t* residual, int32_t zp_r,
+                       float mul_r, int32_t zp_y, int32_t bits, int8_t* y) {
+    if (T < 0 || N < 1 || K < 1 || bits < 2 || bits > 8 || act < 0 || act > 2) return ORACLE_ERR_ARG;
+    if (T == 0) return ORACLE_OK;
+    int32_t* acc = (int32_t*)malloc(sizeof(int32_t) * (size_t)T * (size_t)N);
+    if (!acc) return ORACLE_ERR_ARG;
+    const int rc = oracle_linear_int32(x, T, w, N, K, fold, acc);
+    const long double lo = -(1 << (bits - 1)), hi = (1 << (bits - 1)) - 1;
+    for (int64_t i = 0; rc == ORACLE_OK && i < T * N; ++i) {
+        const long double a = (float)acc[i], m = mul[i % N];
+        long double v = a * m;
+        if (act == 1 && v < 0) v = 0;
+        if (act == 2) {
+            const long double last = (1 << table_bits) - 1;
+            v = table[(int)clip_ld(rintl(a * m + zp_t), 0, last)];
+        }
+        if (residual) {
+            const float c = (float)((long double)zp_y - (128 + zp_r) * (long double)mul_r);
+            const float z = (float)(((int)residual[i] + 128) * (long double)mul_r + c);
+            if (act == 1) v = (float)v;
+            v = (float)(v + z);
+        } else {
+            v += zp_y;
+        }
+        y[i] = (int8_t)clip_ld(rintl(v), lo, hi);
+    }
+    free(acc);
+    return rc;
+}
+
+/* One entry per token and pair: (cos, sin) of position times frequency in
+ * steps of 2^-14. */
+int oracle_rope_table_int16(const int32_t* positions, int32_t axes, int64_t T, const double* freq,
+                            const uint8_t* axis, int32_t P, int16_t* table) {
+    if (axes < 1 || T < 0 || P < 1) return ORACLE_ERR_ARG;
+    for (int64_t t = 0; t < T; ++t)
+        for (int32_t p = 0; p < P; ++p) {
+            const int64_t ax = axis[p] < axes ? axis[p] : axes - 1;
+            const double angle = (double)positions[ax * T + t] * freq[p];
+            table[(t * P + p) * 2] = (int16_t)rint(16384.0 * cos(angle));
+            table[(t * P + p) * 2 + 1] = (int16_t)rint(16384.0 * sin(angle));
+        }
+    return ORACLE_OK;
+}
+
+/* Rows [B, L, (Hq + 2 Hkv) d] into heads; queries and keys turned by the table
+ * and requantized, values copied. */
+int oracle_rope_qkv_int8(const int8_t* qkv, int64_t B, int32_t L, int32_t Hq, int32_t Hkv,
+                         int32_t d, float s_x, int32_t zp_x, const int16_t* table,
+                         int64_t table_rows, int32_t P, int32_t interleaved, float s_q, int32_t zp_q,
+                         float s_k, int32_t zp_k, int32_t bits, int8_t* q, int8_t* k, int8_t* v) {
+    const int32_t heads = Hq + 2 * Hkv;
+    const long double lo = -(1 << (bits - 1)), hi = (1 << (bits - 1)) - 1;
+    int64_t f[256];
+    if (d > 256 || 2 * P > d) return ORACLE_ERR_ARG;
+    for (int64_t b = 0; b < B; ++b)
+        for (int64_t l = 0; l < L; ++l)
+            for (int64_t h = 0; h < heads; ++h) {
+                const int8_t* row = qkv + ((b * L + l) * heads + h) * d;
+                if (h >= Hq + Hkv) {
+                    memcpy(v + ((b * Hkv + h - Hq - Hkv) * L + l) * d, row, (size_t)d);
+                    continue;
+                }
+                for (int32_t j = 0; j < d; ++j) f[j] = ((int64_t)row[j] - zp_x) * 16384;
+                for (int32_t p = 0; p < P; ++p) {
+                    const int32_t i0 = interleaved ? 2 * p : p, i1 = interleaved ? 2 * p + 1 : p + P;
+                    const int64_t at = ((table_rows == L ? l : b * L + l) * P + p) * 2;
+                    const int64_t c = table[at], s = table[at + 1];
+                    const int64_t x0 = (int64_t)row[i0] - zp_x, x1 = (int64_t)row[i1] - zp_x;
+                    f[i0] = x0 * c - x1 * s;
+                    f[i1] = x0 * s + x1 * c;
+                }
+                const int is_q = h < Hq;
+                double m = (double)s_x / (16384.0 * (double)(is_q ? s_q : s_k));
+                if (m > 3.4028234663852886e38) m = 3.4028234663852886e38;
+                int8_t* out = is_q ? q + ((b * Hq + h) * L + l) * d : k + ((b * Hkv + h - Hq) * L + l) * d;
+                for (int32_t j = 0; j < d; ++j)
+                    out[j] = (int8_t)clip_ld(rintl((long double)f[j] * (float)m + (is_q ? zp_q : zp_k)),
+                                             lo, hi);
+            }
+    return ORACLE_OK;
+}
+
+/* oracle_requant_dyadic_int8 of q [B, H, L, d], stored as [B, L, H, d]. */
+int oracle_requant_heads_int8(const int32_t* q, int64_t B, int32_t H, int32_t L, int32_t d,
+                              float s_in, float s_out, int32_t zp_out, int32_t bits, int8_t* y) {
+    for (int64_t b = 0; b < B; ++b)
+        for (int64_t h = 0; h < H; ++h)
+            for (int64_t l = 0; l < L; ++l) {
+                const int rc = oracle_requant_dyadic_int8(q + ((b * H + h) * L + l) * d, d, s_in, s_out,
+                                                          zp_out, bits, y + ((b * L + l) * H + h) * d);
+                if (rc != ORACLE_OK) return rc;
+            }
+    return ORACLE_OK;
+}

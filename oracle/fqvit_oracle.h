@@ -150,6 +150,29 @@ int oracle_lis_attention_qk(const int8_t* q, const int8_t* k, int32_t zp_q, int3
                             int32_t Lk, float s_logit, int32_t bits, int32_t exp_n,
                             const int8_t* v, int32_t zp_v, int32_t d, int32_t* out);
 
+/* ---- Linear layers (Sec. 3.1), rotary positions, heads back to rows ------ */
+
+/* Folded bias and per-channel multipliers; mul nullable. */
+int oracle_linear_fold_int8(const int8_t* w, int32_t N, int32_t K, const float* s_w,
+                            const float* bias, int32_t zp_x, float s_x, float s_y, int32_t* fold,
+                            float* mul);
+/* x [T, K] w [N, K]^T + fold, exact; ORACLE_ERR_RANGE if a sum leaves int32. */
+int oracle_linear_int32(const int8_t* x, int64_t T, const int8_t* w, int32_t N, int32_t K,
+                        const int32_t* fold, int32_t* out);
+/* The same requantized; act 0 none, 1 ReLU, 2 table; residual nullable. */
+int oracle_linear_int8(const int8_t* x, int64_t T, const int8_t* w, int32_t N, int32_t K,
+                       const int32_t* fold, const float* mul, int32_t act, const float* table,
+                       int32_t table_bits, int32_t zp_t, const int8_t* residual, int32_t zp_r,
+                       float mul_r, int32_t zp_y, int32_t bits, int8_t* y);
+int oracle_rope_table_int16(const int32_t* positions, int32_t axes, int64_t T, const double* freq,
+                            const uint8_t* axis, int32_t P, int16_t* table);
+int oracle_rope_qkv_int8(const int8_t* qkv, int64_t B, int32_t L, int32_t Hq, int32_t Hkv,
+                         int32_t d, float s_x, int32_t zp_x, const int16_t* table,
+                         int64_t table_rows, int32_t P, int32_t interleaved, float s_q, int32_t zp_q,
+                         float s_k, int32_t zp_k, int32_t bits, int8_t* q, int8_t* k, int8_t* v);
+int oracle_requant_heads_int8(const int32_t* q, int64_t B, int32_t H, int32_t L, int32_t d,
+                              float s_in, float s_out, int32_t zp_out, int32_t bits, int8_t* y);
+
 #ifdef __cplusplus
 }
 #endif

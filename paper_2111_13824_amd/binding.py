@@ -36,7 +36,19 @@ SIGNATURES = {
     "ptf_calibrate_noalloc": [_P, _I64, _I32, _I32, _I32, _P, _P, _P, _P],
     "ptf_quantize_int8": [_P, _I64, _I32, _P, _P, _P, _I32, _P, _P],
     "requant_dyadic_int8": [_P, _I64, _F32, _F32, _I32, _I32, _P, _P],
+    "linear_fold_int8": [_P, _I32, _I32, _P, _P, _I32, _F32, _F32, _P, _P, _P],
+    "linear_int8": [_P, _I64, _P, _I32, _I32, _P, _P, _I32, _P, _I32, _I32, _P, _I32, _F32, _I32,
+                    _I32, _P, _P],
+    "linear_int32": [_P, _I64, _P, _I32, _I32, _P, _P, _P],
+    "rope_table_int16": [_P, _I32, _I64, _P, _P, _I32, _P, _P],
+    "rope_qkv_int8": [_P, _I64, _I32, _I32, _I32, _I32, _F32, _I32, _P, _I64, _I32, _I32, _F32,
+                      _I32, _F32, _I32, _I32, _P, _P, _P, _P],
+    "requant_heads_int8": [_P, _I64, _I32, _I32, _I32, _F32, _F32, _I32, _I32, _P, _P],
+    "fq_activation_table": [_I32, _F32, _I32, _I32, _F32, _P],
 }
+# Activations of linear_int8 and functions of fq_activation_table.
+ACT_NONE, ACT_RELU, ACT_TABLE = range(3)
+_FUNCTIONS = {"gelu": 0, "gelu_tanh": 1, "silu": 2}
 
 
 class FqError(RuntimeError):
@@ -128,29 +140,51 @@ class Prepared:
     """A validated call with its arguments already converted to C types:
     calling it only enters the library (for launch loops where Python
     marshalling would otherwise dominate).  The stream is the one current when
-    the call was prepared; the tensors are kept alive by the object."""
+    the call was prepared; the tensors are kept alive by the object.  With
+    `device`, the call runs with that device current (a default stream is the
+    current device's)."""
 
-    __slots__ = ("_name", "_fn", "_args", "_keep")
+    __slots__ = ("_name", "_fn", "_args", "_keep", "_device")
 
-    def __init__(self, name: str, args, keep):
+    def __init__(self, name: str, args, keep, device: Optional[int] = None):
         self._name = name
         self._fn = getattr(lib(), name)
         self._args = tuple(t(a) if a is not None else None
                            for t, a in zip(SIGNATURES[name], args))
         self._keep = keep
+        self._device = device
 
     def __call__(self) -> None:
-        st = self._fn(*self._args)
+        st = _enter(self._fn, self._args, self._device)
         if st != FQ_OK:
             raise FqError(self._name, st)
 
 
-def _invoke(name: str, args, keep, prepare: bool, result):
+def _enter(fn, args, device: Optional[int]) -> int:
+    """fn(*args), with `device` current where one is given."""
+    if device is None:
+        return fn(*args)
+    import torch
+    if torch._C._cuda_getDevice() == device:
+        return fn(*args)
+    with torch.cuda.device(device):
+        return fn(*args)
+
+
+def _invoke(name: str, args, keep, prepare: bool, result, device: Optional[int] = None):
     """Run the entry point now, or return it prepared for repeated calls."""
     if prepare:
-        return Prepared(name, args, keep)
-    _check(name, getattr(lib(), name)(*args))
+        return Prepared(name, args, keep, device)
+    _check(name, _enter(getattr(lib(), name), args, device))
     return result
+
+
+def _one_device(like, **tensors) -> int:
+    """The index of the device that tensor `like` and all the others lie on."""
+    for name, t in tensors.items():
+        if t is not None and t.device != like.device:
+            raise ValueError(f"{name} must be on {like.device}, got {t.device}")
+    return like.device.index
 
 
 def ptf_layernorm_int8(x_q, zp_in: int, alpha, K: int, gamma, beta, s_out: float, zp_out: int,
@@ -355,3 +389,154 @@ def lis_attention_qk(q, k, v, s_logit: float, zp_q: int = 0, zp_k: int = 0, bits
             _dev_ptr(v, torch.int8, "v", 3), zp_v, d, _dev_ptr(out, torch.int32, "out", 3),
             _stream(stream, q))
     return _invoke("lis_attention_qk", args, (q, k, v, bias, out), prepare, out)
+
+
+def linear_fold_int8(w, s_w, s_x: float, s_y: float = 1.0, zp_x: int = 0, bias=None, fold=None,
+                     mul=None, stream=None, prepare: bool = False):
+    """What a linear layer's products take besides its int8 weights w [N, K]:
+    (fold, mul), the folded bias (int32 [N]) and the channels' multipliers
+    (float [N]), from the weight scales s_w [N], the input's scale and zero
+    point, the float bias [N] and the output's step s_y (the table's step where
+    an activation table follows).  Once for a layer."""
+    import torch
+    N, K = w.shape
+    fold = torch.empty(N, dtype=torch.int32, device=w.device) if fold is None else fold
+    mul = torch.empty(N, dtype=torch.float32, device=w.device) if mul is None else mul
+    if s_w.shape != (N,) or fold.shape != (N,) or mul.shape != (N,) or \
+            (bias is not None and bias.shape != (N,)):
+        raise ValueError("s_w, bias, fold and mul must be [N]")
+    args = (_dev_ptr(w, torch.int8, "w", 2), N, K, _dev_ptr(s_w, torch.float32, "s_w", 1),
+            _dev_ptr(bias, torch.float32, "bias", 1), zp_x, s_x, s_y,
+            _dev_ptr(fold, torch.int32, "fold", 1), _dev_ptr(mul, torch.float32, "mul", 1),
+            _stream(stream, w))
+    return _invoke("linear_fold_int8", args, (w, s_w, bias, fold, mul), prepare, (fold, mul),
+                   _one_device(w, s_w=s_w, bias=bias, fold=fold, mul=mul))
+
+
+def linear_int8(x, w, fold, mul, zp_y: int = 0, bits: int = 8, relu: bool = False, table=None,
+                zp_t: Optional[int] = None, residual=None, zp_r: int = 0, mul_r: float = 1.0,
+                y=None, stream=None, prepare: bool = False):
+    """Linear layer with its epilogue: int8 [T, N] from int8 x [T, K] and w [N, K]
+    with fold and mul of linear_fold_int8.  relu, or an activation table
+    (activation_table; zp_t defaults to its middle); residual int8 [T, N] with
+    zero point zp_r and mul_r = s_r / s_y is added after the activation.  y may
+    be the residual."""
+    import torch
+    T, K = x.shape
+    N = w.shape[0]
+    if y is None:
+        y = torch.empty((T, N), dtype=torch.int8, device=x.device)
+    if w.shape != (N, K) or mul.shape != (N,) or (fold is not None and fold.shape != (N,)):
+        raise ValueError("w must be [N, K], fold and mul [N]")
+    if y.shape != (T, N) or (residual is not None and residual.shape != (T, N)):
+        raise ValueError("y and residual must be [T, N]")
+    act, table_bits = ACT_NONE, 0
+    if table is not None:
+        if relu:
+            raise ValueError("give relu or a table, not both")
+        act, table_bits = ACT_TABLE, table.numel().bit_length() - 1
+        if table.numel() != 1 << table_bits:
+            raise ValueError("table must hold a power of two of values")
+        zp_t = (1 << table_bits) >> 1 if zp_t is None else zp_t
+    elif relu:
+        act = ACT_RELU
+    args = (_dev_ptr(x, torch.int8, "x", 2), T, _dev_ptr(w, torch.int8, "w", 2), N, K,
+            _dev_ptr(fold, torch.int32, "fold", 1), _dev_ptr(mul, torch.float32, "mul", 1), act,
+            _dev_ptr(table, torch.float32, "table", 1), table_bits, zp_t or 0,
+            _dev_ptr(residual, torch.int8, "residual", 2), zp_r, mul_r, zp_y, bits,
+            _dev_ptr(y, torch.int8, "y", 2), _stream(stream, x))
+    return _invoke("linear_int8", args, (x, w, fold, mul, table, residual, y), prepare, y,
+                   _one_device(x, w=w, fold=fold, mul=mul, table=table, residual=residual, y=y))
+
+
+def linear_int32(x, w, fold=None, out=None, stream=None, prepare: bool = False):
+    """The linear layer's accumulators: int32 [T, N] = x w^T + fold."""
+    import torch
+    T, K = x.shape
+    N = w.shape[0]
+    if out is None:
+        out = torch.empty((T, N), dtype=torch.int32, device=x.device)
+    if w.shape != (N, K) or (fold is not None and fold.shape != (N,)) or out.shape != (T, N):
+        raise ValueError("w must be [N, K], fold [N] and out [T, N]")
+    args = (_dev_ptr(x, torch.int8, "x", 2), T, _dev_ptr(w, torch.int8, "w", 2), N, K,
+            _dev_ptr(fold, torch.int32, "fold", 1), _dev_ptr(out, torch.int32, "out", 2),
+            _stream(stream, x))
+    return _invoke("linear_int32", args, (x, w, fold, out), prepare, out,
+                   _one_device(x, w=w, fold=fold, out=out))
+
+
+def activation_table(kind: str, s_t: float, s_y: float, zp_t: Optional[int] = None,
+                     table_bits: int = 10, device="cuda"):
+    """An activation ("gelu", "gelu_tanh" or "silu") as a table for linear_int8:
+    its values in steps s_y of the output over the grid s_t (u - zp_t) of
+    2^table_bits inputs (zp_t defaults to the middle)."""
+    import torch
+    if kind not in _FUNCTIONS:
+        raise ValueError(f"kind must be one of {', '.join(_FUNCTIONS)}")
+    if not 4 <= table_bits <= 12:
+        raise ValueError("table_bits must be in [4, 12]")
+    host = torch.empty(1 << table_bits, dtype=torch.float32)
+    zp_t = (1 << table_bits) >> 1 if zp_t is None else zp_t
+    _check("fq_activation_table",
+           lib().fq_activation_table(_FUNCTIONS[kind], s_t, zp_t, table_bits, s_y, host.data_ptr()))
+    return host.to(device)
+
+
+def rope_table_int16(positions, freq, axis, table=None, stream=None, prepare: bool = False):
+    """cos and sin of positions int32 [axes, T] times freq float64 [P], pair p
+    along axis[p] (uint8 [P]), in steps of 2^-14: int16 [T, P, 2]."""
+    import torch
+    axes, T = positions.shape
+    P = freq.shape[0]
+    if table is None:
+        table = torch.empty((T, P, 2), dtype=torch.int16, device=positions.device)
+    if axis.shape != (P,) or table.shape != (T, P, 2):
+        raise ValueError("axis must be [P] and table [T, P, 2]")
+    args = (_dev_ptr(positions, torch.int32, "positions", 2), axes, T,
+            _dev_ptr(freq, torch.float64, "freq", 1), _dev_ptr(axis, torch.uint8, "axis", 1), P,
+            _dev_ptr(table, torch.int16, "table", 3), _stream(stream, positions))
+    return _invoke("rope_table_int16", args, (positions, freq, axis, table), prepare, table,
+                   _one_device(positions, freq=freq, axis=axis, table=table))
+
+
+def rope_qkv_int8(qkv, table, Hq: int, Hkv: int, s_x: float, s_q: float, s_k: float, zp_x: int = 0,
+                  zp_q: int = 0, zp_k: int = 0, bits: int = 8, interleaved: bool = False, q=None,
+                  k=None, v=None, stream=None, prepare: bool = False):
+    """The query-key-value layer's int8 rows [B, L, (Hq + 2 Hkv) d] split into
+    heads, queries and keys rotated by the table (int16 [L or B L, P, 2]; None:
+    no rotation) and requantized: (q [B, Hq, L, d], k and v [B, Hkv, L, d])."""
+    import torch
+    B, L, row = qkv.shape
+    heads = Hq + 2 * Hkv
+    if Hq < 1 or Hkv < 1 or row % heads:
+        raise ValueError("qkv must be [B, L, (Hq + 2 Hkv) d]")
+    d = row // heads
+    rows, P = (table.shape[0], table.shape[1]) if table is not None else (0, 0)
+    if table is not None and (table.dim() != 3 or table.shape[2] != 2):
+        raise ValueError("table must be [L or B L, P, 2]")
+    q = torch.empty((B, Hq, L, d), dtype=torch.int8, device=qkv.device) if q is None else q
+    k = torch.empty((B, Hkv, L, d), dtype=torch.int8, device=qkv.device) if k is None else k
+    v = torch.empty((B, Hkv, L, d), dtype=torch.int8, device=qkv.device) if v is None else v
+    if q.shape != (B, Hq, L, d) or k.shape != (B, Hkv, L, d) or v.shape != (B, Hkv, L, d):
+        raise ValueError("q must be [B, Hq, L, d], k and v [B, Hkv, L, d]")
+    args = (_dev_ptr(qkv, torch.int8, "qkv", 3), B, L, Hq, Hkv, d, s_x, zp_x,
+            _dev_ptr(table, torch.int16, "table", 3), rows, P, int(interleaved), s_q, zp_q, s_k,
+            zp_k, bits, _dev_ptr(q, torch.int8, "q", 4), _dev_ptr(k, torch.int8, "k", 4),
+            _dev_ptr(v, torch.int8, "v", 4), _stream(stream, qkv))
+    return _invoke("rope_qkv_int8", args, (qkv, table, q, k, v), prepare, (q, k, v),
+                   _one_device(qkv, table=table, q=q, k=k, v=v))
+
+
+def requant_heads_int8(q, s_in: float, s_out: float, zp_out: int, bits: int = 8, y=None,
+                       stream=None, prepare: bool = False):
+    """Dyadic requantization of an attention result int32 [B, H, L, d] with its
+    heads brought back to rows: int8 [B, L, H d]."""
+    import torch
+    B, H, L, d = q.shape
+    if y is None:
+        y = torch.empty((B, L, H * d), dtype=torch.int8, device=q.device)
+    if y.shape != (B, L, H * d):
+        raise ValueError("y must be [B, L, H d]")
+    args = (_dev_ptr(q, torch.int32, "q", 4), B, H, L, d, s_in, s_out, zp_out, bits,
+            _dev_ptr(y, torch.int8, "y", 3), _stream(stream, q))
+    return _invoke("requant_heads_int8", args, (q, y), prepare, y, _one_device(q, y=y))

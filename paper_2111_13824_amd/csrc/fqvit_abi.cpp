@@ -81,6 +81,46 @@ bool grid_fits(int64_t G, int32_t Lq, int32_t rows_per_block) {
     return G <= (int64_t)0x7FFFFFFF / (tiles > 0 ? tiles : 1);
 }
 
+// N2 / 2^N1: the 31-bit dyadic form of M = s_in / s_out.
+void dyadic(float s_in, float s_out, int64_t* n2, int32_t* n1) {
+    const double M = (double)s_in / (double)s_out;
+    int e = 0;
+    (void)std::frexp(M, &e);
+    int64_t N1 = 31 - (int64_t)e;
+    N1 = N1 < 0 ? 0 : (N1 > 62 ? 62 : N1);
+    double m = std::floor(std::ldexp(M, (int)N1));
+    if (m > 2147483647.0) m = 2147483647.0;
+    *n2 = (int64_t)m;
+    *n1 = (int32_t)N1;
+}
+
+constexpr int32_t kMaxN = 1 << 20;      // output channels of a linear layer
+// Products of (x - zp) w, |.| <= 255 * 128, of this many inputs stay below 2^30,
+// as the folded bias does: every accumulator fits int32.
+constexpr int32_t kMaxK = 32768;
+
+constexpr int32_t kMaxHeads = 1024;
+
+// num / den as a binary32 multiplier (at most the largest finite one).
+float multiplier(double num, double den) {
+    return (float)std::fmin(num / den, 3.4028234663852886e38);
+}
+
+bool positive(float s) { return s > 0.0f && std::isfinite(s); }
+bool int8_zp(int32_t zp) { return zp >= -128 && zp <= 127; }
+
+// Sizes of a linear product.  The smallest tile is 16 x 16.
+bool linear_sizes(int64_t T, int32_t N, int32_t K) {
+    if (T < 0 || T > ((int64_t)1 << 40) || N < 1 || N > kMaxN || K < 1 || K > kMaxK) return false;
+    return ((T + 15) / 16) <= (int64_t)0x7FFFFFFF / ((N + 15) / 16);
+}
+
+// The launch, where this build has its kernels.
+template <typename A>
+fq_status launched(hipError_t (*launch)(const A&, hipStream_t), const A& a, void* stream) {
+    return launch ? from_hip(launch(a, (hipStream_t)stream)) : FQ_ERR_HIP;
+}
+
 }  // namespace
 
 // Workspace of the calibration: the min/max partials, the per-block error sums
@@ -313,16 +353,185 @@ fq_status requant_dyadic_int8(const int32_t* q, int64_t n, float s_in, float s_o
     if (zp_out < -half || zp_out >= half) return FQ_ERR_PARAM;
     if (n == 0) return FQ_OK;
     if (!q || !y) return FQ_ERR_NULL;
-    // N2 / 2^N1: the 31-bit dyadic form of M = s_in / s_out.
-    const double M = (double)s_in / (double)s_out;
-    int e = 0;
-    (void)std::frexp(M, &e);
-    int64_t N1 = 31 - (int64_t)e;
-    N1 = N1 < 0 ? 0 : (N1 > 62 ? 62 : N1);
-    double n2 = std::floor(std::ldexp(M, (int)N1));
-    if (n2 > 2147483647.0) n2 = 2147483647.0;
-    fqvit::RequantArgs a{q, n, (int64_t)n2, (int32_t)N1, zp_out, bits, y};
+    int64_t n2;
+    int32_t n1;
+    dyadic(s_in, s_out, &n2, &n1);
+    fqvit::RequantArgs a{q, n, n2, n1, zp_out, bits, y};
     return from_hip(fqvit::launch_requant(a, (hipStream_t)stream));
+}
+
+fq_status linear_fold_int8(const int8_t* w, int32_t N, int32_t K, const float* s_w,
+                           const float* bias, int32_t zp_x, float s_x, float s_y, int32_t* fold,
+                           float* mul, void* stream) {
+    ConsumeEvents consume;
+    if (!linear_sizes(1, N, K)) return FQ_ERR_SHAPE;
+    if (!int8_zp(zp_x) || !positive(s_x) || (mul && !positive(s_y))) return FQ_ERR_PARAM;
+    if (!w || !s_w || !fold) return FQ_ERR_NULL;
+    const fqvit::LinearFoldArgs a{w, N, K, s_w, bias, zp_x, s_x, s_y, fold, mul};
+    return launched(fqvit::launch_linear_fold, a, stream);
+}
+
+fq_status linear_int8(const int8_t* x, int64_t T, const int8_t* w, int32_t N, int32_t K,
+                      const int32_t* fold, const float* mul, int32_t act, const float* table,
+                      int32_t table_bits, int32_t zp_t, const int8_t* residual, int32_t zp_r,
+                      float mul_r, int32_t zp_y, int32_t bits, int8_t* y, void* stream) {
+    ConsumeEvents consume;
+    if (!linear_sizes(T, N, K)) return FQ_ERR_SHAPE;
+    if (act != FQ_ACT_NONE && act != FQ_ACT_RELU && act != FQ_ACT_TABLE) return FQ_ERR_PARAM;
+    if (act == FQ_ACT_TABLE &&
+        (table_bits < 4 || table_bits > 12 || zp_t < 0 || zp_t >= (1 << table_bits)))
+        return FQ_ERR_PARAM;
+    if (residual && (!int8_zp(zp_r) || !(mul_r >= 0x1p-20f && mul_r <= 0x1p20f)))
+        return FQ_ERR_PARAM;
+    if (bits < 2 || bits > 8) return FQ_ERR_PARAM;
+    const int32_t half = 1 << (bits - 1);
+    if (zp_y < -half || zp_y >= half) return FQ_ERR_PARAM;
+    if (T == 0) return FQ_OK;
+    if (!x || !w || !mul || !y || (act == FQ_ACT_TABLE && !table)) return FQ_ERR_NULL;
+    fqvit::LinearArgs a{};
+    a.x = x;
+    a.w = w;
+    a.fold = fold;
+    a.mul = mul;
+    a.T = T;
+    a.N = N;
+    a.K = K;
+    a.act = act;
+    if (act == FQ_ACT_TABLE) {
+        a.table = table;
+        a.table_bits = table_bits;
+        a.zp_t = zp_t;
+    }
+    if (residual) {
+        a.residual = residual;
+        a.mul_r = mul_r;
+        // 8 + 24 bits: the product and the difference are exact in binary64
+        a.add_r = (float)((double)zp_y - (double)(128 + zp_r) * (double)mul_r);
+    }
+    a.zp_y = zp_y;
+    a.bits = bits;
+    a.y = y;
+    return launched(fqvit::launch_linear, a, stream);
+}
+
+fq_status linear_int32(const int8_t* x, int64_t T, const int8_t* w, int32_t N, int32_t K,
+                       const int32_t* fold, int32_t* out, void* stream) {
+    ConsumeEvents consume;
+    if (!linear_sizes(T, N, K)) return FQ_ERR_SHAPE;
+    if (T == 0) return FQ_OK;
+    if (!x || !w || !out) return FQ_ERR_NULL;
+    fqvit::LinearArgs a{};
+    a.x = x;
+    a.w = w;
+    a.fold = fold;
+    a.T = T;
+    a.N = N;
+    a.K = K;
+    a.acc = out;
+    return launched(fqvit::launch_linear, a, stream);
+}
+
+fq_status fq_activation_table(int32_t kind, float s_t, int32_t zp_t, int32_t table_bits, float s_y,
+                              float* table) {
+    if (kind < FQ_FN_GELU || kind > FQ_FN_SILU || table_bits < 4 || table_bits > 12 || zp_t < 0 ||
+        zp_t >= (1 << table_bits) || !positive(s_t) || !positive(s_y))
+        return FQ_ERR_PARAM;
+    if (!table) return FQ_ERR_NULL;
+    auto value = [=](int u) {
+        const double t = (double)s_t * (u - zp_t);
+        double f;
+        if (kind == FQ_FN_GELU)
+            f = 0.5 * t * (1.0 + std::erf(t * 0.70710678118654752440));
+        else if (kind == FQ_FN_GELU_TANH)
+            f = 0.5 * t *
+                (1.0 + std::tanh(0.79788456080286535588 * (t + 0.044715 * t * t * t)));
+        else
+            f = t < -700.0 ? 0.0 : t / (1.0 + std::exp(-t));   // exp's range ends at 709
+        return f / (double)s_y;
+    };
+    // the magnitude grows towards the two ends
+    const int last = (1 << table_bits) - 1;
+    if (!(std::fabs(value(0)) <= 3.4e38) || !(std::fabs(value(last)) <= 3.4e38)) return FQ_ERR_PARAM;
+    for (int u = 0; u <= last; ++u) table[u] = (float)value(u);
+    return FQ_OK;
+}
+
+fq_status rope_table_int16(const int32_t* positions, int32_t axes, int64_t T, const double* freq,
+                           const uint8_t* axis, int32_t P, int16_t* table, void* stream) {
+    ConsumeEvents consume;
+    if (T < 0 || T > 0x7FFFFFFF || axes < 1 || axes > 8 || P < 1 || P > kMaxD / 2)
+        return FQ_ERR_SHAPE;
+    if (T == 0) return FQ_OK;
+    if (!positions || !freq || !axis || !table) return FQ_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(table) & 3) != 0) return FQ_ERR_PARAM;
+    const fqvit::RopeTableArgs a{positions, axes, T, freq, axis, P, table};
+    return launched(fqvit::launch_rope_table, a, stream);
+}
+
+fq_status rope_qkv_int8(const int8_t* qkv, int64_t B, int32_t L, int32_t Hq, int32_t Hkv, int32_t d,
+                        float s_x, int32_t zp_x, const int16_t* table, int64_t table_rows, int32_t P,
+                        int32_t interleaved, float s_q, int32_t zp_q, float s_k, int32_t zp_k,
+                        int32_t bits, int8_t* q, int8_t* k, int8_t* v, void* stream) {
+    ConsumeEvents consume;
+    if (B < 0 || L < 0 || Hq < 1 || Hq > kMaxHeads || Hkv < 1 || Hkv > kMaxHeads || d < 1 ||
+        d > kMaxD || P < 0 || P > d / 2 || (L > 0 && B > (int64_t)0x7FFFFFFF / L))
+        return FQ_ERR_SHAPE;
+    if (P > 0 && table_rows != L && table_rows != B * L) return FQ_ERR_SHAPE;
+    if (bits < 2 || bits > 8 || (interleaved != 0 && interleaved != 1)) return FQ_ERR_PARAM;
+    const int32_t half = 1 << (bits - 1);
+    if (!int8_zp(zp_x) || zp_q < -half || zp_q >= half || zp_k < -half || zp_k >= half)
+        return FQ_ERR_PARAM;
+    if (!positive(s_x) || !positive(s_q) || !positive(s_k)) return FQ_ERR_PARAM;
+    if (B == 0 || L == 0) return FQ_OK;
+    if (!qkv || !q || !k || !v || (P > 0 && !table)) return FQ_ERR_NULL;
+    if (P > 0 && (reinterpret_cast<uintptr_t>(table) & 3) != 0) return FQ_ERR_PARAM;
+    fqvit::RopeArgs a{};
+    a.qkv = qkv;
+    a.B = B;
+    a.L = L;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.d = d;
+    a.zp_x = zp_x;
+    a.table = table;
+    a.per_image = table_rows != L;
+    a.P = P;
+    a.interleaved = interleaved;
+    a.m_q = multiplier((double)s_x, 16384.0 * (double)s_q);
+    a.m_k = multiplier((double)s_x, 16384.0 * (double)s_k);
+    a.zp_q = zp_q;
+    a.zp_k = zp_k;
+    a.bits = bits;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    return launched(fqvit::launch_rope_qkv, a, stream);
+}
+
+fq_status requant_heads_int8(const int32_t* q, int64_t B, int32_t H, int32_t L, int32_t d,
+                             float s_in, float s_out, int32_t zp_out, int32_t bits, int8_t* y,
+                             void* stream) {
+    ConsumeEvents consume;
+    if (B < 0 || L < 0 || H < 1 || H > kMaxHeads || d < 1 || d > kMaxD ||
+        (L > 0 && B > (int64_t)0x7FFFFFFF / L))
+        return FQ_ERR_SHAPE;
+    if (bits < 2 || bits > 8) return FQ_ERR_PARAM;
+    if (!positive(s_in) || !positive(s_out)) return FQ_ERR_PARAM;
+    const int32_t half = 1 << (bits - 1);
+    if (zp_out < -half || zp_out >= half) return FQ_ERR_PARAM;
+    if (B == 0 || L == 0) return FQ_OK;
+    if (!q || !y) return FQ_ERR_NULL;
+    fqvit::RequantHeadsArgs a{};
+    a.r.q = q;
+    dyadic(s_in, s_out, &a.r.N2, &a.r.N1);
+    a.r.zp = zp_out;
+    a.r.bits = bits;
+    a.r.y = y;
+    a.B = B;
+    a.H = H;
+    a.L = L;
+    a.d = d;
+    return launched(fqvit::launch_requant_heads, a, stream);
 }
 
 }  // extern "C"

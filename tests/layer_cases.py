@@ -1,0 +1,81 @@
+"""Inputs and plain 64-bit forms for the tests of the linear layers, the rotary
+positions and the heads' way back to rows.  The plain forms are numpy, written
+from the definitions in include/fqvit.h; integer products go through binary64,
+where sums of int8 products are exact."""
+import numpy as np
+
+
+def f32(v):
+    """Rounded to the nearest binary32, as binary64."""
+    return np.asarray(v, np.float64).astype(np.float32).astype(np.float64)
+
+
+def fold(w, s_w, s_x, s_y=1.0, zp_x=0, bias=None):
+    s_n = float(np.float32(s_x)) * s_w.astype(np.float64)
+    b = np.zeros(len(w)) if bias is None else np.rint(bias.astype(np.float64) / s_n)
+    b = np.clip(b, -2.0 ** 30, 2.0 ** 30)
+    rows = w.astype(np.int64).sum(1)
+    return ((b.astype(np.int64) - zp_x * rows).astype(np.int32),
+            (s_n / float(np.float32(s_y))).astype(np.float32))
+
+
+def sums(x, w, fold_=None):
+    s = x.astype(np.float64) @ w.astype(np.float64).T
+    return s if fold_ is None else s + fold_
+
+
+def linear(x, w, fold_, mul, zp_y=0, bits=8, relu=False, table=None, zp_t=0, residual=None, zp_r=0,
+           mul_r=1.0):
+    a, m = f32(sums(x, w, fold_)), mul.astype(np.float64)
+    v = a * m
+    if table is not None:
+        v = table.astype(np.float64)[np.clip(np.rint(v + zp_t), 0, len(table) - 1).astype(np.int64)]
+    elif relu:
+        v = np.maximum(f32(v) if residual is not None else v, 0)
+    if residual is None:
+        v = v + zp_y
+    else:
+        mr = float(np.float32(mul_r))
+        v = f32(v + f32((residual.astype(np.float64) + 128) * mr + f32(zp_y - (128 + zp_r) * mr)))
+    half = 1 << (bits - 1)
+    return np.clip(np.rint(v), -half, half - 1).astype(np.int8)
+
+
+def rope_table(positions, freq, axis):
+    t = positions[np.minimum(axis, len(positions) - 1)].T.astype(np.float64) * freq
+    return np.rint(16384.0 * np.stack((np.cos(t), np.sin(t)), -1)).astype(np.int16)
+
+
+def rope(qkv, table, Hq, Hkv, s_x, s_q, s_k, zp_x=0, zp_q=0, zp_k=0, bits=8, interleaved=False):
+    B, L, row = qkv.shape
+    heads = Hq + 2 * Hkv
+    x = qkv.reshape(B, L, heads, row // heads)
+    f = (x.astype(np.int64) - zp_x)
+    out = f * 16384
+    if table is not None:
+        P = table.shape[1]
+        at = np.arange(P)
+        one, two = (2 * at, 2 * at + 1) if interleaved else (at, at + P)
+        c, s = table.astype(np.int64).reshape(-1, L, 1, P, 2).transpose(4, 0, 1, 2, 3)
+        out[..., one] = f[..., one] * c - f[..., two] * s
+        out[..., two] = f[..., one] * s + f[..., two] * c
+    half = 1 << (bits - 1)
+
+    def grid(part, scale, zp):
+        m = f32(float(np.float32(s_x)) / (16384.0 * float(np.float32(scale))))
+        return np.clip(np.rint(part * m + zp), -half, half - 1).astype(np.int8).transpose(0, 2, 1, 3)
+
+    return (grid(out[:, :, :Hq], s_q, zp_q), grid(out[:, :, Hq:Hq + Hkv], s_k, zp_k),
+            x[:, :, Hq + Hkv:].transpose(0, 2, 1, 3))
+
+
+def layer(T, K, N, seed, zp_x=0, spread=36.0):
+    """A quantized layer's inputs: x, w, weight scales, bias and scales that fill
+    the output grid."""
+    g = np.random.default_rng(seed)
+    x = np.clip(np.rint(g.normal(zp_x, spread, (T, K))), -128, 127).astype(np.int8)
+    w = np.clip(np.rint(g.normal(0, 40, (N, K))), -128, 127).astype(np.int8)
+    s_x = np.float32(0.02)
+    s_w = (np.exp(g.uniform(-0.7, 0.7, N)) * 1.5 / (s_x * spread * 40 * np.sqrt(K))).astype(np.float32)
+    bias = g.normal(0, 0.3, N).astype(np.float32)
+    return dict(x=x, w=w, s_w=s_w, bias=bias, s_x=float(s_x), s_y=9.0 / 255, zp_x=zp_x)

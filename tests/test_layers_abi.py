@@ -1,0 +1,253 @@
+"""Refusals of the linear layers, the rotary positions and the heads' way back
+to rows, in the C ABI and in the binding, and the constants that the host
+derives.  Every call here fails its checks, is empty, or runs against a host
+build whose launchers only keep their arguments (built with AddressSanitizer
+and UndefinedBehaviorSanitizer where the environment variable names one)."""
+import ctypes
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+
+from paper_2111_13824_amd import binding as B
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+SAN_LIB = os.environ.get("FQVIT_LAYER_TEST_LIB")
+
+
+def host_library(out, flags=()):
+    csrc = os.path.join(ROOT, "paper_2111_13824_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-fPIC", "-shared", *flags, "-D__HIP_PLATFORM_AMD__",
+                    "-I/opt/rocm/include", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                    os.path.join(csrc, "fqvit_abi.cpp"), os.path.join(HERE, "abi_launch_stubs.cpp"),
+                    os.path.join(HERE, "layer_launch_stubs.cpp"), "-o", out], check=True)
+    return out
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    return B.load(SAN_LIB or host_library(str(tmp_path_factory.mktemp("host") / "libhost.so")))
+
+
+def caller(lib, name, **defaults):
+    """call(**changes): the entry point with its arguments, some changed, and
+    whether it reached its launcher."""
+    def call(**kw):
+        assert set(kw) <= set(defaults), kw
+        n = lib.fq_test_layer_calls()
+        rc = getattr(lib, name)(*dict(defaults, **kw).values(), None)
+        return rc, lib.fq_test_layer_calls() - n
+    return call
+
+
+RAN, EMPTY = (B.FQ_OK, 1), (B.FQ_OK, 0)
+NULL, SHAPE, PARAM = (B.FQ_ERR_NULL, 0), (B.FQ_ERR_SHAPE, 0), (B.FQ_ERR_PARAM, 0)
+
+
+def test_fold_refusals(lib):
+    call = caller(lib, "linear_fold_int8", w=1, N=8, K=16, s_w=1, bias=None, zp=0, s_x=0.5, s_y=0.5,
+                  fold=1, mul=1)
+    assert call() == RAN and call(bias=1) == RAN and call(K=32768, N=1 << 20) == RAN
+    assert call(mul=None, s_y=0.0) == RAN           # without multipliers the step is unused
+    for k, v in (("N", 0), ("N", (1 << 20) + 1), ("K", 0), ("K", 32769), ("N", -1)):
+        assert call(**{k: v}) == SHAPE
+    for k, v in (("zp", 128), ("zp", -129), ("s_x", 0.0), ("s_x", float("inf")), ("s_y", -1.0),
+                 ("s_y", float("nan"))):
+        assert call(**{k: v}) == PARAM
+    for k in ("w", "s_w", "fold"):
+        assert call(**{k: None}) == NULL
+
+
+def test_linear_refusals(lib):
+    call = caller(lib, "linear_int8", x=1, T=4, w=1, N=8, K=16, fold=1, mul=1, act=0, table=None,
+                  tbits=0, zp_t=0, res=None, zp_r=0, mul_r=1.0, zp=0, bits=8, y=1)
+    assert call() == RAN and call(fold=None) == RAN and call(act=1) == RAN
+    assert call(act=2, table=1, tbits=4, zp_t=15) == RAN and call(res=1, zp_r=-128) == RAN
+    assert call(T=0, x=None, y=None) == EMPTY
+    # what is not used is not looked at
+    assert call(tbits=99, zp_t=-5, zp_r=1000, mul_r=0.0) == RAN
+    for k, v in (("T", -1), ("N", 0), ("K", 0), ("K", 32769), ("N", (1 << 20) + 1), ("T", 1 << 41)):
+        assert call(**{k: v}) == SHAPE
+    assert call(T=1 << 24, N=1 << 20) == SHAPE      # more tiles than a grid holds
+    for k, v in (("act", 3), ("act", -1), ("bits", 1), ("bits", 9), ("zp", 128), ("zp", -129)):
+        assert call(**{k: v}) == PARAM
+    assert call(bits=4, zp=8) == PARAM
+    for k, v in (("tbits", 3), ("tbits", 13), ("zp_t", -1), ("zp_t", 16)):
+        assert call(**dict(dict(act=2, table=1, tbits=4), **{k: v})) == PARAM
+    for k, v in (("zp_r", 128), ("zp_r", -129), ("mul_r", 0.0), ("mul_r", float("nan")),
+                 ("mul_r", 2.0 ** 21), ("mul_r", -1.0)):
+        assert call(res=1, **{k: v}) == PARAM
+    for k in ("x", "w", "mul", "y"):
+        assert call(**{k: None}) == NULL
+    assert call(act=2, tbits=4) == NULL
+
+
+def test_linear_int32_refusals(lib):
+    call = caller(lib, "linear_int32", x=1, T=4, w=1, N=8, K=16, fold=1, out=1)
+    assert call() == RAN and call(fold=None) == RAN and call(T=0, x=None) == EMPTY
+    for k, v in (("T", -1), ("N", 0), ("K", 0), ("K", 32769)):
+        assert call(**{k: v}) == SHAPE
+    for k in ("x", "w", "out"):
+        assert call(**{k: None}) == NULL
+
+
+def test_rope_refusals(lib):
+    call = caller(lib, "rope_table_int16", pos=1, axes=3, T=5, freq=1, axis=1, P=4, table=4)
+    assert call() == RAN and call(T=0, pos=None) == EMPTY
+    for k, v in (("axes", 0), ("axes", 9), ("T", -1), ("T", 1 << 31), ("P", 0), ("P", 129)):
+        assert call(**{k: v}) == SHAPE
+    assert call(table=2) == PARAM
+    for k in ("pos", "freq", "axis", "table"):
+        assert call(**{k: None}) == NULL
+
+    call = caller(lib, "rope_qkv_int8", qkv=1, B=2, L=5, Hq=4, Hkv=2, d=64, s_x=0.5, zp_x=0, table=4,
+                  rows=5, P=32, il=0, s_q=0.5, zp_q=0, s_k=0.5, zp_k=0, bits=8, q=1, k=1, v=1)
+    assert call() == RAN and call(rows=10, il=1) == RAN and call(P=0, table=None, rows=0) == RAN
+    assert call(B=0, qkv=None) == EMPTY and call(L=0, rows=0, q=None) == EMPTY
+    for k, v in (("B", -1), ("L", -1), ("Hq", 0), ("Hkv", 0), ("Hq", 1025), ("d", 0), ("d", 257),
+                 ("P", -1), ("P", 33), ("rows", 4), ("rows", 6), ("rows", 20), ("B", 1 << 40)):
+        assert call(**{k: v}) == SHAPE, (k, v)
+    for k, v in (("il", 2), ("bits", 1), ("bits", 9), ("zp_x", 128), ("zp_q", 128), ("zp_k", -129),
+                 ("s_x", 0.0), ("s_q", float("nan")), ("s_k", float("inf")), ("table", 6)):
+        assert call(**{k: v}) == PARAM, (k, v)
+    assert call(bits=4, zp_q=8) == PARAM and call(bits=4, zp_k=-9) == PARAM
+    for k in ("qkv", "q", "k", "v", "table"):
+        assert call(**{k: None}) == NULL
+
+
+def test_requant_heads_refusals(lib):
+    call = caller(lib, "requant_heads_int8", q=1, B=2, H=3, L=5, d=64, si=0.5, so=0.25, zp=0, bits=8,
+                  y=1)
+    assert call() == RAN and call(B=0, q=None) == EMPTY and call(L=0, y=None) == EMPTY
+    for k, v in (("B", -1), ("H", 0), ("H", 1025), ("L", -1), ("d", 0), ("d", 257), ("B", 1 << 40)):
+        assert call(**{k: v}) == SHAPE
+    for k, v in (("si", 0.0), ("so", float("inf")), ("bits", 1), ("bits", 9), ("zp", 128)):
+        assert call(**{k: v}) == PARAM
+    assert call(q=None) == NULL and call(y=None) == NULL
+
+
+def test_derived_constants(lib):
+    """add_r and the rotation's multipliers, rounded once; the dyadic form."""
+    f, i = np.zeros(3, np.float32), np.zeros(3, np.int64)
+    for zp_r, mul_r, zp in ((0, 0.3, 0), (-128, 7.0, 5), (127, 2.0 ** -20 * 1.3, -128)):
+        assert caller(lib, "linear_int8", x=1, T=4, w=1, N=8, K=16, fold=1, mul=1, act=0, table=None,
+                      tbits=0, zp_t=0, res=1, zp_r=zp_r, mul_r=mul_r, zp=zp, bits=8, y=1)() == RAN
+        lib.fq_test_multipliers(f.ctypes.data_as(ctypes.c_void_p))
+        assert f[0] == np.float32(zp - (128 + zp_r) * float(np.float32(mul_r)))
+    rope = caller(lib, "rope_qkv_int8", qkv=1, B=2, L=5, Hq=4, Hkv=2, d=64, s_x=0.05, zp_x=0, table=4,
+                  rows=5, P=32, il=0, s_q=0.07, zp_q=0, s_k=1e-38, zp_k=0, bits=8, q=1, k=1, v=1)
+    assert rope(s_x=3e38) == RAN                    # the ratio leaves binary32
+    lib.fq_test_multipliers(f.ctypes.data_as(ctypes.c_void_p))
+    assert f[2] == np.finfo(np.float32).max
+    assert rope(rows=10) == RAN
+    lib.fq_test_multipliers(f.ctypes.data_as(ctypes.c_void_p))
+    lib.fq_test_integers(i.ctypes.data_as(ctypes.c_void_p))
+    assert f[1] == np.float32(float(np.float32(0.05)) / (16384 * float(np.float32(0.07))))
+    assert i[2] == 1
+    assert caller(lib, "requant_heads_int8", q=1, B=2, H=3, L=5, d=64, si=0.75, so=1.0, zp=0, bits=8,
+                  y=1)() == RAN
+    lib.fq_test_integers(i.ctypes.data_as(ctypes.c_void_p))
+    assert (i[0], i[1]) == (3 << 29, 31)
+
+
+def test_a_build_without_the_kernels_says_so(tmp_path):
+    """The host code alone loads; a call that needs a missing kernel returns a
+    status instead of ending the process."""
+    csrc = os.path.join(ROOT, "paper_2111_13824_amd", "csrc")
+    out = str(tmp_path / "libalone.so")
+    subprocess.run(["g++", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__",
+                    "-I/opt/rocm/include", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                    os.path.join(csrc, "fqvit_abi.cpp"), os.path.join(HERE, "abi_launch_stubs.cpp"),
+                    "-o", out], check=True)
+    alone = B.load(out)
+    assert alone.linear_int32(1, 4, 1, 8, 16, None, 1, None) == B.FQ_ERR_HIP
+    assert alone.rope_table_int16(1, 1, 5, 1, 1, 4, 4, None) == B.FQ_ERR_HIP
+
+
+def test_activation_tables(lib):
+    from math import erf, exp, tanh, pi, sqrt
+    f = {0: lambda t: t * (1 + erf(t / sqrt(2))) / 2,
+         1: lambda t: t * (1 + tanh(sqrt(2 / pi) * (t + 0.044715 * t ** 3))) / 2,
+         2: lambda t: t / (1 + exp(-t))}
+    for kind in f:
+        for bits, zp, s_t, s_y in ((4, 0, 0.5, 0.25), (10, 512, 1 / 64, 0.05), (12, 4095, 0.004, 1e-3)):
+            table = np.zeros((1 << bits) + 1, np.float32)
+            assert lib.fq_activation_table(kind, s_t, zp, bits, s_y, table.ctypes.data) == B.FQ_OK
+            t = float(np.float32(s_t)) * (np.arange(1 << bits) - zp)
+            ref = np.array([f[kind](v) for v in t]) / float(np.float32(s_y))
+            # rounding to binary32 (half a step) and a few roundings in binary64;
+            # 1 + erf and 1 + tanh cancel below 0, to within t 2^-53 / s_y
+            assert np.all(np.abs(table[:-1] - ref) <= np.abs(ref) * 2.0 ** -24 * 1.01 +
+                          np.abs(t) * 2.0 ** -50 / s_y + 2.0 ** -149)
+            assert table[-1] == 0
+    table = np.zeros(16, np.float32)
+    assert lib.fq_activation_table(2, 1e4, 8, 4, 1.0, table.ctypes.data) == B.FQ_OK
+    assert np.all(table[:9] == 0) and table[9] == 1e4   # far below 0 SiLU is 0
+    for args in ((3, 1.0, 0, 4, 1.0), (-1, 1.0, 0, 4, 1.0), (0, 0.0, 0, 4, 1.0), (0, 1.0, 16, 4, 1.0),
+                 (0, 1.0, -1, 4, 1.0), (0, 1.0, 0, 3, 1.0), (0, 1.0, 0, 13, 1.0),
+                 (0, 1.0, 0, 4, float("nan")), (0, 3e38, 0, 4, 1e-3)):
+        assert lib.fq_activation_table(*args, table.ctypes.data) == B.FQ_ERR_PARAM
+    assert lib.fq_activation_table(0, 1.0, 0, 4, 1.0, None) == B.FQ_ERR_NULL
+
+
+@pytest.mark.skipif(bool(SAN_LIB), reason="needs torch, which the sanitizer run leaves out")
+def test_binding_refusals(lib, monkeypatch):
+    torch = pytest.importorskip("torch")
+    import paper_2111_13824_amd as fq
+    monkeypatch.setattr(B, "_lib", lib)
+    i8, f32, i32 = torch.int8, torch.float32, torch.int32
+    x, w = torch.zeros(4, 8, dtype=i8), torch.zeros(3, 8, dtype=i8)
+    fold, mul = torch.zeros(3, dtype=i32), torch.zeros(3)
+    with pytest.raises(ValueError, match="device tensor"):
+        fq.linear_int8(x, w, fold, mul)
+    with pytest.raises(TypeError, match="int8"):
+        fq.linear_int8(x.float(), w, fold, mul)
+    with pytest.raises(ValueError, match=r"\[N, K\]"):
+        fq.linear_int8(x, w[:, :7], fold, mul)
+    with pytest.raises(ValueError, match=r"fold and mul"):
+        fq.linear_int8(x, w, fold[:2], mul)
+    with pytest.raises(ValueError, match="residual must be"):
+        fq.linear_int8(x, w, fold, mul, residual=x)
+    with pytest.raises(ValueError, match="not both"):
+        fq.linear_int8(x, w, fold, mul, relu=True, table=torch.zeros(16))
+    with pytest.raises(ValueError, match="power of two"):
+        fq.linear_int8(x, w, fold, mul, table=torch.zeros(17))
+    with pytest.raises(ValueError, match=r"out \[T, N\]"):
+        fq.linear_int32(x, w, fold, out=torch.zeros(4, 4, dtype=i32))
+    with pytest.raises(ValueError, match=r"must be \[N\]"):
+        fq.linear_fold_int8(w, torch.zeros(4, dtype=f32), 1.0)
+    with pytest.raises(ValueError, match="kind"):
+        fq.activation_table("tan", 1.0, 1.0, device="cpu")
+    with pytest.raises(ValueError, match="table_bits"):
+        fq.activation_table("gelu", 1.0, 1.0, table_bits=20, device="cpu")
+    with pytest.raises(B.FqError):
+        fq.activation_table("gelu", 0.0, 1.0, device="cpu")
+    assert fq.activation_table("silu", 0.5, 1.0, device="cpu")[512] == 0
+    pos = torch.zeros(3, 5, dtype=i32)
+    with pytest.raises(ValueError, match=r"axis must be \[P\]"):
+        fq.rope_table_int16(pos, torch.zeros(4, dtype=torch.float64), torch.zeros(3, dtype=torch.uint8))
+    qkv, table = torch.zeros(2, 5, 32, dtype=i8), torch.zeros(5, 4, 2, dtype=torch.int16)
+    with pytest.raises(ValueError, match="qkv must be"):
+        fq.rope_qkv_int8(qkv, table, 3, 1, 1.0, 1.0, 1.0)
+    with pytest.raises(ValueError, match="table must be"):
+        fq.rope_qkv_int8(qkv, table[..., :1], 2, 1, 1.0, 1.0, 1.0)
+    with pytest.raises(ValueError, match="q must be"):
+        fq.rope_qkv_int8(qkv, table, 2, 1, 1.0, 1.0, 1.0, q=torch.zeros(2, 2, 5, 9, dtype=i8))
+    with pytest.raises(ValueError, match="y must be"):
+        fq.requant_heads_int8(torch.zeros(2, 3, 5, 8, dtype=i32), 1.0, 1.0, 0,
+                              y=torch.zeros(2, 5, 25, dtype=i8))
+
+
+@pytest.mark.skipif(bool(SAN_LIB), reason="this is the run that starts it")
+def test_host_code_under_sanitizers(tmp_path):
+    from test_sanitizers import SAN, _env
+    env = _env({"FQVIT_LAYER_TEST_LIB": host_library(str(tmp_path / "libsan.so"), SAN)})
+    r = subprocess.run([sys.executable, "-m", "pytest", os.path.abspath(__file__), "-q", "-s", "-p",
+                        "no:cacheprovider"], cwd=ROOT, env=env, capture_output=True, text=True,
+                       timeout=600)
+    out = r.stdout + r.stderr
+    assert "AddressSanitizer" not in out and "runtime error" not in out, out[-4000:]
+    assert r.returncode == 0 and " passed" in out, out[-4000:]
