@@ -179,12 +179,45 @@ def _invoke(name: str, args, keep, prepare: bool, result, device: Optional[int] 
     return result
 
 
-def _one_device(like, **tensors) -> int:
-    """The index of the device that tensor `like` and all the others lie on."""
-    for name, t in tensors.items():
-        if t is not None and t.device != like.device:
-            raise ValueError(f"{name} must be on {like.device}, got {t.device}")
-    return like.device.index
+def _device_of(t, name: str) -> int:
+    """The index of the device that tensor `t` lies on."""
+    try:
+        device = t.get_device()
+    except AttributeError:
+        raise TypeError(f"{name} must be a torch.Tensor") from None
+    if device < 0:
+        raise ValueError(f"{name} must be a device tensor")
+    return device
+
+
+def _arg(t, dtype, shape, device: int, name: str):
+    """The address of tensor `t` (None for None), which has to be contiguous, of
+    this dtype and shape, on this device."""
+    if t is None:
+        return None
+    try:
+        if (t.dtype is dtype and t.shape == shape and t.get_device() == device
+                and t.is_contiguous()):
+            return t.data_ptr()
+    except AttributeError:
+        raise TypeError(f"{name} must be a torch.Tensor") from None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.get_device() < 0:
+        raise ValueError(f"{name} must be a device tensor")
+    raise ValueError(f"{name} must be on device {device}, got {t.device}")
+
+
+def _dims(t, n: int, name: str):
+    """The shape of tensor `t`, which has to have n dimensions."""
+    shape = t.shape
+    if len(shape) != n:
+        raise ValueError(f"{name} must have {n} dimensions, got {len(shape)}")
+    return shape
 
 
 def ptf_layernorm_int8(x_q, zp_in: int, alpha, K: int, gamma, beta, s_out: float, zp_out: int,
@@ -399,18 +432,17 @@ def linear_fold_int8(w, s_w, s_x: float, s_y: float = 1.0, zp_x: int = 0, bias=N
     point, the float bias [N] and the output's step s_y (the table's step where
     an activation table follows).  Once for a layer."""
     import torch
-    N, K = w.shape
-    fold = torch.empty(N, dtype=torch.int32, device=w.device) if fold is None else fold
-    mul = torch.empty(N, dtype=torch.float32, device=w.device) if mul is None else mul
-    if s_w.shape != (N,) or fold.shape != (N,) or mul.shape != (N,) or \
-            (bias is not None and bias.shape != (N,)):
-        raise ValueError("s_w, bias, fold and mul must be [N]")
-    args = (_dev_ptr(w, torch.int8, "w", 2), N, K, _dev_ptr(s_w, torch.float32, "s_w", 1),
-            _dev_ptr(bias, torch.float32, "bias", 1), zp_x, s_x, s_y,
-            _dev_ptr(fold, torch.int32, "fold", 1), _dev_ptr(mul, torch.float32, "mul", 1),
+    N, K = _dims(w, 2, "w")
+    dev = _device_of(w, "w")
+    if fold is None:
+        fold = torch.empty(N, dtype=torch.int32, device=w.device)
+    if mul is None:
+        mul = torch.empty(N, dtype=torch.float32, device=w.device)
+    args = (_arg(w, torch.int8, (N, K), dev, "w"), N, K, _arg(s_w, torch.float32, (N,), dev, "s_w"),
+            _arg(bias, torch.float32, (N,), dev, "bias"), zp_x, s_x, s_y,
+            _arg(fold, torch.int32, (N,), dev, "fold"), _arg(mul, torch.float32, (N,), dev, "mul"),
             _stream(stream, w))
-    return _invoke("linear_fold_int8", args, (w, s_w, bias, fold, mul), prepare, (fold, mul),
-                   _one_device(w, s_w=s_w, bias=bias, fold=fold, mul=mul))
+    return _invoke("linear_fold_int8", args, (w, s_w, bias, fold, mul), prepare, (fold, mul), dev)
 
 
 def linear_int8(x, w, fold, mul, zp_y: int = 0, bits: int = 8, relu: bool = False, table=None,
@@ -422,47 +454,43 @@ def linear_int8(x, w, fold, mul, zp_y: int = 0, bits: int = 8, relu: bool = Fals
     zero point zp_r and mul_r = s_r / s_y is added after the activation.  y may
     be the residual."""
     import torch
-    T, K = x.shape
+    i8, f32 = torch.int8, torch.float32
+    T, K = _dims(x, 2, "x")
     N = w.shape[0]
-    if y is None:
-        y = torch.empty((T, N), dtype=torch.int8, device=x.device)
-    if w.shape != (N, K) or mul.shape != (N,) or (fold is not None and fold.shape != (N,)):
-        raise ValueError("w must be [N, K], fold and mul [N]")
-    if y.shape != (T, N) or (residual is not None and residual.shape != (T, N)):
-        raise ValueError("y and residual must be [T, N]")
-    act, table_bits = ACT_NONE, 0
+    dev = _device_of(x, "x")
+    act, bits_t, size = ACT_NONE, 0, 0
     if table is not None:
         if relu:
             raise ValueError("give relu or a table, not both")
-        act, table_bits = ACT_TABLE, table.numel().bit_length() - 1
-        if table.numel() != 1 << table_bits:
+        act, size = ACT_TABLE, table.numel()
+        bits_t = size.bit_length() - 1
+        if size != 1 << bits_t:
             raise ValueError("table must hold a power of two of values")
-        zp_t = (1 << table_bits) >> 1 if zp_t is None else zp_t
+        zp_t = size >> 1 if zp_t is None else zp_t
     elif relu:
         act = ACT_RELU
-    args = (_dev_ptr(x, torch.int8, "x", 2), T, _dev_ptr(w, torch.int8, "w", 2), N, K,
-            _dev_ptr(fold, torch.int32, "fold", 1), _dev_ptr(mul, torch.float32, "mul", 1), act,
-            _dev_ptr(table, torch.float32, "table", 1), table_bits, zp_t or 0,
-            _dev_ptr(residual, torch.int8, "residual", 2), zp_r, mul_r, zp_y, bits,
-            _dev_ptr(y, torch.int8, "y", 2), _stream(stream, x))
-    return _invoke("linear_int8", args, (x, w, fold, mul, table, residual, y), prepare, y,
-                   _one_device(x, w=w, fold=fold, mul=mul, table=table, residual=residual, y=y))
+    px = _arg(x, i8, (T, K), dev, "x")
+    if y is None:
+        y = x.new_empty((T, N))
+    args = (px, T, _arg(w, i8, (N, K), dev, "w"), N, K, _arg(fold, torch.int32, (N,), dev, "fold"),
+            _arg(mul, f32, (N,), dev, "mul"), act, _arg(table, f32, (size,), dev, "table"), bits_t,
+            zp_t or 0, _arg(residual, i8, (T, N), dev, "residual"), zp_r, mul_r, zp_y, bits,
+            _arg(y, i8, (T, N), dev, "y"), _stream(stream, x))
+    return _invoke("linear_int8", args, (x, w, fold, mul, table, residual, y), prepare, y, dev)
 
 
 def linear_int32(x, w, fold=None, out=None, stream=None, prepare: bool = False):
     """The linear layer's accumulators: int32 [T, N] = x w^T + fold."""
     import torch
-    T, K = x.shape
+    T, K = _dims(x, 2, "x")
     N = w.shape[0]
+    dev = _device_of(x, "x")
     if out is None:
         out = torch.empty((T, N), dtype=torch.int32, device=x.device)
-    if w.shape != (N, K) or (fold is not None and fold.shape != (N,)) or out.shape != (T, N):
-        raise ValueError("w must be [N, K], fold [N] and out [T, N]")
-    args = (_dev_ptr(x, torch.int8, "x", 2), T, _dev_ptr(w, torch.int8, "w", 2), N, K,
-            _dev_ptr(fold, torch.int32, "fold", 1), _dev_ptr(out, torch.int32, "out", 2),
+    args = (_arg(x, torch.int8, (T, K), dev, "x"), T, _arg(w, torch.int8, (N, K), dev, "w"), N, K,
+            _arg(fold, torch.int32, (N,), dev, "fold"), _arg(out, torch.int32, (T, N), dev, "out"),
             _stream(stream, x))
-    return _invoke("linear_int32", args, (x, w, fold, out), prepare, out,
-                   _one_device(x, w=w, fold=fold, out=out))
+    return _invoke("linear_int32", args, (x, w, fold, out), prepare, out, dev)
 
 
 def activation_table(kind: str, s_t: float, s_y: float, zp_t: Optional[int] = None,
@@ -486,17 +514,15 @@ def rope_table_int16(positions, freq, axis, table=None, stream=None, prepare: bo
     """cos and sin of positions int32 [axes, T] times freq float64 [P], pair p
     along axis[p] (uint8 [P]), in steps of 2^-14: int16 [T, P, 2]."""
     import torch
-    axes, T = positions.shape
-    P = freq.shape[0]
+    axes, T = _dims(positions, 2, "positions")
+    P, = _dims(freq, 1, "freq")
+    dev = _device_of(positions, "positions")
     if table is None:
         table = torch.empty((T, P, 2), dtype=torch.int16, device=positions.device)
-    if axis.shape != (P,) or table.shape != (T, P, 2):
-        raise ValueError("axis must be [P] and table [T, P, 2]")
-    args = (_dev_ptr(positions, torch.int32, "positions", 2), axes, T,
-            _dev_ptr(freq, torch.float64, "freq", 1), _dev_ptr(axis, torch.uint8, "axis", 1), P,
-            _dev_ptr(table, torch.int16, "table", 3), _stream(stream, positions))
-    return _invoke("rope_table_int16", args, (positions, freq, axis, table), prepare, table,
-                   _one_device(positions, freq=freq, axis=axis, table=table))
+    args = (_arg(positions, torch.int32, (axes, T), dev, "positions"), axes, T,
+            _arg(freq, torch.float64, (P,), dev, "freq"), _arg(axis, torch.uint8, (P,), dev, "axis"),
+            P, _arg(table, torch.int16, (T, P, 2), dev, "table"), _stream(stream, positions))
+    return _invoke("rope_table_int16", args, (positions, freq, axis, table), prepare, table, dev)
 
 
 def rope_qkv_int8(qkv, table, Hq: int, Hkv: int, s_x: float, s_q: float, s_k: float, zp_x: int = 0,
@@ -506,25 +532,26 @@ def rope_qkv_int8(qkv, table, Hq: int, Hkv: int, s_x: float, s_q: float, s_k: fl
     heads, queries and keys rotated by the table (int16 [L or B L, P, 2]; None:
     no rotation) and requantized: (q [B, Hq, L, d], k and v [B, Hkv, L, d])."""
     import torch
-    B, L, row = qkv.shape
+    i8 = torch.int8
+    B, L, row = _dims(qkv, 3, "qkv")
     heads = Hq + 2 * Hkv
     if Hq < 1 or Hkv < 1 or row % heads:
         raise ValueError("qkv must be [B, L, (Hq + 2 Hkv) d]")
     d = row // heads
-    rows, P = (table.shape[0], table.shape[1]) if table is not None else (0, 0)
-    if table is not None and (table.dim() != 3 or table.shape[2] != 2):
-        raise ValueError("table must be [L or B L, P, 2]")
-    q = torch.empty((B, Hq, L, d), dtype=torch.int8, device=qkv.device) if q is None else q
-    k = torch.empty((B, Hkv, L, d), dtype=torch.int8, device=qkv.device) if k is None else k
-    v = torch.empty((B, Hkv, L, d), dtype=torch.int8, device=qkv.device) if v is None else v
-    if q.shape != (B, Hq, L, d) or k.shape != (B, Hkv, L, d) or v.shape != (B, Hkv, L, d):
-        raise ValueError("q must be [B, Hq, L, d], k and v [B, Hkv, L, d]")
-    args = (_dev_ptr(qkv, torch.int8, "qkv", 3), B, L, Hq, Hkv, d, s_x, zp_x,
-            _dev_ptr(table, torch.int16, "table", 3), rows, P, int(interleaved), s_q, zp_q, s_k,
-            zp_k, bits, _dev_ptr(q, torch.int8, "q", 4), _dev_ptr(k, torch.int8, "k", 4),
-            _dev_ptr(v, torch.int8, "v", 4), _stream(stream, qkv))
-    return _invoke("rope_qkv_int8", args, (qkv, table, q, k, v), prepare, (q, k, v),
-                   _one_device(qkv, table=table, q=q, k=k, v=v))
+    dev = _device_of(qkv, "qkv")
+    rows, P = (0, 0) if table is None else _dims(table, 3, "table")[:2]
+    sq, sk = (B, Hq, L, d), (B, Hkv, L, d)
+    px = _arg(qkv, i8, (B, L, row), dev, "qkv")
+    if q is None:
+        q = qkv.new_empty(sq)
+    if k is None:
+        k = qkv.new_empty(sk)
+    if v is None:
+        v = qkv.new_empty(sk)
+    args = (px, B, L, Hq, Hkv, d, s_x, zp_x, _arg(table, torch.int16, (rows, P, 2), dev, "table"),
+            rows, P, 1 if interleaved else 0, s_q, zp_q, s_k, zp_k, bits, _arg(q, i8, sq, dev, "q"),
+            _arg(k, i8, sk, dev, "k"), _arg(v, i8, sk, dev, "v"), _stream(stream, qkv))
+    return _invoke("rope_qkv_int8", args, (qkv, table, q, k, v), prepare, (q, k, v), dev)
 
 
 def requant_heads_int8(q, s_in: float, s_out: float, zp_out: int, bits: int = 8, y=None,
@@ -532,11 +559,11 @@ def requant_heads_int8(q, s_in: float, s_out: float, zp_out: int, bits: int = 8,
     """Dyadic requantization of an attention result int32 [B, H, L, d] with its
     heads brought back to rows: int8 [B, L, H d]."""
     import torch
-    B, H, L, d = q.shape
+    B, H, L, d = _dims(q, 4, "q")
+    dev = _device_of(q, "q")
+    shape = (B, L, H * d)
     if y is None:
-        y = torch.empty((B, L, H * d), dtype=torch.int8, device=q.device)
-    if y.shape != (B, L, H * d):
-        raise ValueError("y must be [B, L, H d]")
-    args = (_dev_ptr(q, torch.int32, "q", 4), B, H, L, d, s_in, s_out, zp_out, bits,
-            _dev_ptr(y, torch.int8, "y", 3), _stream(stream, q))
-    return _invoke("requant_heads_int8", args, (q, y), prepare, y, _one_device(q, y=y))
+        y = torch.empty(shape, dtype=torch.int8, device=q.device)
+    args = (_arg(q, torch.int32, (B, H, L, d), dev, "q"), B, H, L, d, s_in, s_out, zp_out, bits,
+            _arg(y, torch.int8, shape, dev, "y"), _stream(stream, q))
+    return _invoke("requant_heads_int8", args, (q, y), prepare, y, dev)

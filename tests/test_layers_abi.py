@@ -195,30 +195,50 @@ def test_activation_tables(lib):
 
 @pytest.mark.skipif(bool(SAN_LIB), reason="needs torch, which the sanitizer run leaves out")
 def test_binding_refusals(lib, monkeypatch):
+    """Dtypes, shapes, devices and layouts; host tensors pass for the device's
+    once the first check, that there is a device, is out of the way."""
     torch = pytest.importorskip("torch")
     import paper_2111_13824_amd as fq
     monkeypatch.setattr(B, "_lib", lib)
     i8, f32, i32 = torch.int8, torch.float32, torch.int32
-    x, w = torch.zeros(4, 8, dtype=i8), torch.zeros(3, 8, dtype=i8)
-    fold, mul = torch.zeros(3, dtype=i32), torch.zeros(3)
-    with pytest.raises(ValueError, match="device tensor"):
-        fq.linear_int8(x, w, fold, mul)
-    with pytest.raises(TypeError, match="int8"):
+    z = lambda *shape, dtype=i8: torch.zeros(*shape, dtype=dtype)
+    x, w, fold, mul = z(4, 8), z(3, 8), z(3, dtype=i32), z(3, dtype=f32)
+    for call in (lambda: fq.linear_int8(x, w, fold, mul), lambda: fq.linear_int32(x, w),
+                 lambda: fq.linear_fold_int8(w, mul, 1.0),
+                 lambda: fq.rope_table_int16(z(3, 5, dtype=i32), z(4, dtype=torch.float64),
+                                             z(4, dtype=torch.uint8)),
+                 lambda: fq.rope_qkv_int8(z(2, 5, 32), None, 2, 1, 1.0, 1.0, 1.0),
+                 lambda: fq.requant_heads_int8(z(2, 3, 5, 8, dtype=i32), 1.0, 1.0, 0)):
+        with pytest.raises(ValueError, match="device tensor"):
+            call()
+    monkeypatch.setattr(B, "_device_of", lambda t, name: -1)     # the host's, from here on
+    monkeypatch.setattr(B, "_stream", lambda stream, like: 0)
+    with pytest.raises(TypeError, match="x must be torch.int8"):
         fq.linear_int8(x.float(), w, fold, mul)
-    with pytest.raises(ValueError, match=r"\[N, K\]"):
-        fq.linear_int8(x, w[:, :7], fold, mul)
-    with pytest.raises(ValueError, match=r"fold and mul"):
+    with pytest.raises(TypeError, match="mul must be a torch.Tensor"):
+        fq.linear_int8(x, w, fold, [1.0, 2.0, 3.0])
+    with pytest.raises(ValueError, match="x must have 2 dimensions"):
+        fq.linear_int8(x[0], w, fold, mul)
+    with pytest.raises(ValueError, match=r"w must be \[3, 8\], got \[3, 7\]"):
+        fq.linear_int8(x, w[:, :7].contiguous(), fold, mul)
+    with pytest.raises(ValueError, match="x must be contiguous"):
+        fq.linear_int8(z(8, 4).t(), w, fold, mul)
+    with pytest.raises(ValueError, match=r"fold must be \[3\]"):
         fq.linear_int8(x, w, fold[:2], mul)
-    with pytest.raises(ValueError, match="residual must be"):
+    with pytest.raises(ValueError, match=r"residual must be \[4, 3\]"):
         fq.linear_int8(x, w, fold, mul, residual=x)
+    with pytest.raises(ValueError, match=r"y must be \[4, 3\]"):
+        fq.linear_int8(x, w, fold, mul, y=x)
     with pytest.raises(ValueError, match="not both"):
-        fq.linear_int8(x, w, fold, mul, relu=True, table=torch.zeros(16))
+        fq.linear_int8(x, w, fold, mul, relu=True, table=z(16, dtype=f32))
     with pytest.raises(ValueError, match="power of two"):
-        fq.linear_int8(x, w, fold, mul, table=torch.zeros(17))
-    with pytest.raises(ValueError, match=r"out \[T, N\]"):
-        fq.linear_int32(x, w, fold, out=torch.zeros(4, 4, dtype=i32))
-    with pytest.raises(ValueError, match=r"must be \[N\]"):
-        fq.linear_fold_int8(w, torch.zeros(4, dtype=f32), 1.0)
+        fq.linear_int8(x, w, fold, mul, table=z(17, dtype=f32))
+    with pytest.raises(ValueError, match=r"table must be \[16\]"):
+        fq.linear_int8(x, w, fold, mul, table=z(4, 4, dtype=f32))
+    with pytest.raises(ValueError, match=r"out must be \[4, 3\]"):
+        fq.linear_int32(x, w, fold, out=z(4, 4, dtype=i32))
+    with pytest.raises(ValueError, match=r"s_w must be \[3\]"):
+        fq.linear_fold_int8(w, z(4, dtype=f32), 1.0)
     with pytest.raises(ValueError, match="kind"):
         fq.activation_table("tan", 1.0, 1.0, device="cpu")
     with pytest.raises(ValueError, match="table_bits"):
@@ -226,19 +246,21 @@ def test_binding_refusals(lib, monkeypatch):
     with pytest.raises(B.FqError):
         fq.activation_table("gelu", 0.0, 1.0, device="cpu")
     assert fq.activation_table("silu", 0.5, 1.0, device="cpu")[512] == 0
-    pos = torch.zeros(3, 5, dtype=i32)
-    with pytest.raises(ValueError, match=r"axis must be \[P\]"):
-        fq.rope_table_int16(pos, torch.zeros(4, dtype=torch.float64), torch.zeros(3, dtype=torch.uint8))
-    qkv, table = torch.zeros(2, 5, 32, dtype=i8), torch.zeros(5, 4, 2, dtype=torch.int16)
+    with pytest.raises(ValueError, match=r"axis must be \[4\]"):
+        fq.rope_table_int16(z(3, 5, dtype=i32), z(4, dtype=torch.float64), z(3, dtype=torch.uint8))
+    qkv, table = z(2, 5, 32), z(5, 4, 2, dtype=torch.int16)
     with pytest.raises(ValueError, match="qkv must be"):
         fq.rope_qkv_int8(qkv, table, 3, 1, 1.0, 1.0, 1.0)
-    with pytest.raises(ValueError, match="table must be"):
+    with pytest.raises(ValueError, match=r"table must be \[5, 4, 2\]"):
         fq.rope_qkv_int8(qkv, table[..., :1], 2, 1, 1.0, 1.0, 1.0)
-    with pytest.raises(ValueError, match="q must be"):
-        fq.rope_qkv_int8(qkv, table, 2, 1, 1.0, 1.0, 1.0, q=torch.zeros(2, 2, 5, 9, dtype=i8))
-    with pytest.raises(ValueError, match="y must be"):
-        fq.requant_heads_int8(torch.zeros(2, 3, 5, 8, dtype=i32), 1.0, 1.0, 0,
-                              y=torch.zeros(2, 5, 25, dtype=i8))
+    with pytest.raises(ValueError, match=r"q must be \[2, 2, 5, 8\]"):
+        fq.rope_qkv_int8(qkv, table, 2, 1, 1.0, 1.0, 1.0, q=z(2, 2, 5, 9))
+    with pytest.raises(ValueError, match=r"y must be \[2, 5, 24\]"):
+        fq.requant_heads_int8(z(2, 3, 5, 8, dtype=i32), 1.0, 1.0, 0, y=z(2, 5, 25))
+    # a tensor elsewhere
+    monkeypatch.setattr(B, "_device_of", lambda t, name: 3)
+    with pytest.raises(ValueError, match="x must be a device tensor"):
+        fq.linear_int8(x, w, fold, mul)
 
 
 @pytest.mark.skipif(bool(SAN_LIB), reason="this is the run that starts it")
