@@ -17,9 +17,10 @@ SOURCES = ["ptf_layernorm.hip", "lis_attention.hip", "lis_inst_lo.hip", "lis_ins
            "lis_qk_long.hip", "lis_qk_long_float.hip:FQ_QK32_LO",
            "lis_qk_long_float.hip:FQ_QK32_HI", "lis_qk_long_float.hip:FQ_QK64_LO",
            "lis_qk_long_float.hip:FQ_QK64_HI", "lis_attn_v.hip",
-           "linear.hip", "linear_tile.hip:FQ_TILE_W=2", "linear_tile.hip:FQ_TILE_W=3",
-           "linear_tile.hip:FQ_TILE_W=4", "linear_tile.hip:FQ_TILE_W=5",
-           "linear_tile.hip:FQ_TILE_128", "linear_tile.hip:FQ_TILE_64", "heads.hip",
+           "linear.hip", "linear_rows.hip", "linear_tile.hip:FQ_TILE_W=2",
+           "linear_tile.hip:FQ_TILE_W=3", "linear_tile.hip:FQ_TILE_W=4",
+           "linear_tile.hip:FQ_TILE_W=5", "linear_tile.hip:FQ_TILE_128",
+           "linear_tile.hip:FQ_TILE_64", "heads.hip",
            "fqvit_abi.cpp"]     # "file:MACRO": compiled with -DMACRO
 OBJDIR = os.path.join(HERE, "_build")
 

@@ -59,6 +59,11 @@ constexpr Cost kCosts[] = {
     {256, 256, 1, 1.0f, 4.0f, 11.1e-3f}, {256, 320, 1, 1.0f, 6.5f, 12.5e-3f},
 };
 
+// Products of so few rows take the kernel that shares the inputs out among the
+// wavefronts of a workgroup: K = 4096, N = 1024: 4.5 us for one row (9.0 in tiles of
+// 64 x 64), 7.3 for 32 (9.2), 8.5 for 33 (9.3), 9.8 for 48 (9.2).
+constexpr int kFewRows = 32;
+
 int choose(const LinearArgs& a, int shapes) {
     int best = 0;
     float least = 0;
@@ -79,7 +84,9 @@ int choose(const LinearArgs& a, int shapes) {
 
 hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
     using namespace linear;
-    if (a.K % 16 == 0 &&
+    if (a.T <= kFewRows) {
+        launch_rows(a, stream);
+    } else if (a.K % 16 == 0 &&
         ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15) == 0) {
         switch (choose(a, 6)) {
             case 0: launch_tiles<Tile64>(a, stream); break;

@@ -514,7 +514,7 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
 }
 
 // ---------------------------------------------------------------------------
-// Launches (instantiated in linear_tile.hip)
+// Launches (tiles: instantiated in linear_tile.hip)
 // ---------------------------------------------------------------------------
 
 template <int FT>
@@ -526,6 +526,9 @@ typedef Shape<2, 2, 1, 1, 128, 2, false> Tile64R;
 
 template <class S>
 void launch_tiles(const LinearArgs& a, hipStream_t stream);
+
+// A few rows of x (linear_rows.hip).
+void launch_rows(const LinearArgs& a, hipStream_t stream);
 
 }  // namespace linear
 }  // namespace fqvit
