@@ -6,6 +6,7 @@
 // (48 MB) 8.6 to 9.1 us, 5.5 TB/s; a large copy reaches 5.1.
 #include <algorithm>
 
+#include "bytes_device.h"
 #include "fqvit.h"
 #include "fqvit_launch.h"
 #include "requant_device.h"
@@ -63,9 +64,9 @@ __device__ __forceinline__ Bytes<V> load_bytes(const int8_t* at) {
 // The same moved up by n <= V bytes, zeros below.
 template <int V>
 __device__ __forceinline__ Bytes<V> move_up(Bytes<V> b, int n) {
-    unsigned __int128 u = 0;
+    Bytes16 u = {};
     __builtin_memcpy(&u, &b, V);
-    u = n < V ? u << 8 * n : 0;
+    u = bytes_up(u, n);
     __builtin_memcpy(&b, &u, V);
     return b;
 }

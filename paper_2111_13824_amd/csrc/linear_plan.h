@@ -1,0 +1,74 @@
+// Which kernel a linear layer's product takes (host code only).
+#pragma once
+
+#include "fqvit_internal.h"
+
+namespace fqvit {
+namespace linear {
+
+enum Kernel {
+    kRows16,        // linear_rows.hip: up to 16 rows of x, up to 32
+    kRows32,
+    kTile64,        // linear_tile.h: channels x rows 64 x 64, 128 x 128,
+    kTile128,
+    kTileW2,        // 256 x 128, 256 x 192, 256 x 256, 256 x 320
+    kTileW3,
+    kTileW4,
+    kTileW5,
+    kTile64R,       // 64 x 64 and 128 x 128 with the loads through registers
+    kTile128R,
+};
+
+// Products of so few rows take the kernel that shares the inputs out among the
+// wavefronts of a workgroup: K = 4096, N = 1024: 4.5 us for one row (9.0 in tiles of
+// 64 x 64), 7.3 for 32 (9.2), 8.5 for 33 (9.3), 9.8 for 48 (9.2).
+constexpr int kFewRows = 32;
+
+// What a tile costs, fitted to measurements of 130 products (T 64 .. 25088, K 192 ..
+// 4096, N 192 .. 4096): `per` workgroups share a CU; a CU's tiles take per round of
+// `per` fixed + input K microseconds, the share `few` of it at least.  Large tiles
+// move fewer bytes through L2 for a product but fill the last round worse:
+// 9232 x 1024 x 4096 takes 48 us in 464 tiles of 256 x 320 and 55 in 592 of 256 x 256;
+// 9232 x 4096 x 1024 takes 42 us in 196 tiles of 256 x 192 and 45 in 148 of 256 x 256;
+// 12608 x 768 x 2304 takes 31 us in 450 tiles of 256 x 256 and 34 in 360 of 256 x 320;
+// 788 x 768 x 768 takes 4.2 us in 156 tiles of 64 x 64 and 11.8 in 12 of 256 x 256.
+// Over the 130 the choice costs 0.2% more than the fastest tile of each.
+struct Cost {
+    int bn, bt, per;
+    float few, fixed, input;
+};
+constexpr Cost kCosts[] = {
+    {64, 64, 3, 0.52f, 2.8f, 3.9e-3f},   {128, 128, 2, 0.70f, 2.3f, 6.3e-3f},
+    {256, 128, 2, 0.60f, 3.7f, 9.2e-3f}, {256, 192, 1, 1.0f, 2.4f, 7.6e-3f},
+    {256, 256, 1, 1.0f, 3.3f, 8.5e-3f},  {256, 320, 1, 1.0f, 5.2f, 9.6e-3f},
+};
+
+inline int cheapest(int64_t T, int32_t N, int32_t K, int shapes) {
+    int best = 0;
+    float least = 0;
+    for (int i = 0; i < shapes; ++i) {
+        const Cost& c = kCosts[i];
+        const int64_t tiles = ((N + c.bn - 1) / c.bn) * ((T + c.bt - 1) / c.bt);
+        const float share = (float)((tiles + 255) / 256) / (float)c.per;
+        const float cost = (share > c.few ? share : c.few) * (c.fixed + c.input * (float)K);
+        if (i == 0 || cost < least) {
+            best = i;
+            least = cost;
+        }
+    }
+    return best;
+}
+
+// Rows of whole 16-byte units on 16-byte aligned bases can be loaded straight into
+// LDS.
+inline Kernel plan(const LinearArgs& a) {
+    if (a.T <= 16) return kRows16;
+    if (a.T <= kFewRows) return kRows32;
+    const bool units = a.K % 16 == 0 &&
+                       ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15) == 0;
+    return units ? (Kernel)(kTile64 + cheapest(a.T, a.N, a.K, 6))
+                 : (Kernel)(kTile64R + cheapest(a.T, a.N, a.K, 2));
+}
+
+}  // namespace linear
+}  // namespace fqvit

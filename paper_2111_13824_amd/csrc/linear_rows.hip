@@ -93,8 +93,10 @@ void go(const LinearArgs& a, hipStream_t stream) {
                   dim3(64 * kWaves), 0, stream, a);
 }
 
+}  // namespace
+
 template <int FT>
-void rows(const LinearArgs& a, hipStream_t stream) {
+void launch_rows(const LinearArgs& a, hipStream_t stream) {
     const bool res = a.residual != nullptr;
     if (a.acc)
         go<FT, FQ_ACT_NONE, false, true>(a, stream);
@@ -106,11 +108,8 @@ void rows(const LinearArgs& a, hipStream_t stream) {
         res ? go<FT, FQ_ACT_NONE, true, false>(a, stream) : go<FT, FQ_ACT_NONE, false, false>(a, stream);
 }
 
-}  // namespace
-
-void launch_rows(const LinearArgs& a, hipStream_t stream) {
-    a.T <= 16 ? rows<1>(a, stream) : rows<2>(a, stream);
-}
+template void launch_rows<1>(const LinearArgs&, hipStream_t);
+template void launch_rows<2>(const LinearArgs&, hipStream_t);
 
 }  // namespace linear
 }  // namespace fqvit

@@ -2,6 +2,7 @@
 // with bias, activation, residual and requantization in the epilogue).
 #pragma once
 
+#include "bytes_device.h"
 #include "fqvit.h"
 #include "fqvit_launch.h"
 
@@ -106,15 +107,20 @@ __device__ __forceinline__ float byte_of(uint32_t w, int b) {
 // read one unit of sixteen rows and find it in sixteen different columns of a
 // 256-byte line, without a bank conflict, while the stage stays linear in the
 // order in which loads fill it.
-template <int WN_, int WT_, int FN_, int FT_, int STEP_, int NBUF_, bool DMA_>
+template <int WN_, int WT_, int FN_, int FT_, int STEP_, int NBUF_, bool DMA_, int PER>
 struct Shape {
     static constexpr int WN = WN_, WT = WT_, FN = FN_, FT = FT_, STEP = STEP_, NBUF = NBUF_;
     static constexpr bool DMA = DMA_;
     static constexpr int threads = 64 * WN * WT;
+    static constexpr int waves = PER * WN * WT / 4;       // a SIMD: PER workgroups a CU
     static constexpr int BN = 32 * WN * FN, BT = 32 * WT * FT;
     static constexpr int units = STEP / 16;                               // of a row
-    static constexpr int UN = BN * units / threads, UT = BT * units / threads;   // a thread fills
-    static constexpr int bytes = (BN + BT) * STEP;
+    // Loads of a thread a stage; where they come out uneven, a stage has room for
+    // the rows behind the tile that the last ones are for.
+    static constexpr int UN = (BN * units + threads - 1) / threads;
+    static constexpr int UT = (BT * units + threads - 1) / threads;
+    static_assert(BN * units % threads == 0, "whole loads of the weights");
+    static constexpr int bytes = BN * STEP + UT * threads * 16;
     static constexpr int slice = STEP == 128 ? 1 : 2;
 
     // The place in a stage of a row's unit.
@@ -179,7 +185,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const int8_t* m, int64
 
 // One load of 16 bytes a lane from a buffer straight into LDS: the wavefront's
 // lanes one after another from `s` on.
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t m, int8_t* s, int off) {
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t m, int8_t* s, unsigned off) {
     typedef __attribute__((address_space(3))) void* lds_ptr;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(m, (lds_ptr)s, 16, off, 0, 0, 0);
 }
@@ -191,10 +197,9 @@ __device__ __forceinline__ vi4 load_tail(const int8_t* row, int K, int k) {
         __builtin_memcpy(&v, row + k, 16);
     } else if (k < K && K >= 16) {
         // the row's last 16 bytes, moved down by the part that lies before k
-        unsigned __int128 u;
+        Bytes16 u;
         __builtin_memcpy(&u, row + K - 16, 16);
-        u >>= 8 * (k + 16 - K);
-        v = __builtin_bit_cast(vi4, u);
+        v = __builtin_bit_cast(vi4, bytes_down(u, k + 16 - K));
     } else if (k < K) {
         unsigned __int128 u = 0;
 #pragma unroll 1
@@ -220,28 +225,27 @@ __device__ __forceinline__ void store_end(T* y, vi4 v, int count) {
 
 // 16 residuals of a row from channel n on; beyond N they are 0.
 __device__ __forceinline__ vi4 load_end(const int8_t* row, int N, int n) {
-    unsigned __int128 u = 0;
     if (n >= N) return vi4{0, 0, 0, 0};
     if (N >= 16) {
+        Bytes16 u;
         __builtin_memcpy(&u, row + N - 16, 16);
-        u >>= 8 * (n + 16 - N);
-    } else {
-#pragma unroll 1
-        for (int j = N - 1; j >= n; --j) u = u << 8 | (uint8_t)row[j];
+        return __builtin_bit_cast(vi4, bytes_down(u, n + 16 - N));
     }
+    unsigned __int128 u = 0;
+#pragma unroll 1
+    for (int j = N - 1; j >= n; --j) u = u << 8 | (uint8_t)row[j];
     return __builtin_bit_cast(vi4, u);
 }
 
 // DMA: rows of whole 16-byte units on 16-byte aligned bases go straight into
 // LDS; else through registers.
 template <class S, int ACT, bool RES, bool ACC>
-__global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p, int tiles_n,
+__global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(LinearArgs p, int tiles_n,
                                                                     unsigned tiles) {
     constexpr int FN = S::FN, FT = S::FT, STEP = S::STEP, Q = S::STEP / 32;
     // separate arrays: the compiler then waits for the loads into the one that
     // it reads, not for all of them
     __shared__ __align__(16) int8_t s0[S::bytes], s1[S::bytes], s2[S::NBUF == 3 ? S::bytes : 16];
-    __shared__ __align__(16) float muls[ACC ? 4 : S::BN];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     // Workgroups go to the eight dies in turn; each die takes a run of tiles that
     // lie together, channels first, so that its L2 keeps their rows of x.
@@ -253,12 +257,9 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
     const int h = lane >> 5, K = p.K;
     const int nk = (K + STEP - 1) / STEP;
 
-    if constexpr (!ACC)
-        if (t < S::BN) muls[t] = n0 + t < p.N ? p.mul[n0 + t] : 0.0f;
-
     // The accumulators start as the folded bias.
     vi16 acc[FN][FT];
-    {
+    auto start = [&]() __attribute__((always_inline)) {
         const __amdgpu_buffer_rsrc_t fr = __builtin_amdgcn_make_buffer_rsrc(
             (void*)(p.fold ? p.fold : (const int32_t*)p.x), (short)0, p.fold ? p.N * 4 : 0, 0x00020000);
 #pragma unroll
@@ -273,24 +274,27 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[f][g][4 * q + i] = v[i];
             }
-    }
+    };
 
     if constexpr (S::DMA) {
         const __amdgpu_buffer_rsrc_t wr = rows_of(p.w, p.N, n0, K), xr = rows_of(p.x, p.T, t0, K);
+        // an offset outside every buffer: nothing is read, and the loads that
+        // arrive() counts stay the same
+        constexpr unsigned kNone = 0x70000000u;
         constexpr int U = S::UN > S::UT ? S::UN : S::UT;
-        int off[U];
+        unsigned off[U], past = kNone;      // past: of the last loads of x, if uneven
 #pragma unroll
         for (int i = 0; i < U; ++i) off[i] = S::fill_row(t, i) * K + S::fill_unit(t, i) * 16;
+        if (S::fill_row(t, S::UT - 1) < S::BT) past = off[S::UT - 1];
         auto fill = [&](int8_t* s, int k) __attribute__((always_inline)) {
-            // beyond the last stage the offset lies outside both buffers: nothing
-            // is read, and the loads counted by arrive() stay the same
-            const int k0 = k < nk ? k * STEP : 0x70000000;
+            const unsigned k0 = k < nk ? k * STEP : kNone;
 #pragma unroll
             for (int i = 0; i < S::UN; ++i)
                 load_to_lds(wr, s + 16 * (S::threads * i + 64 * wave), off[i] + k0);
 #pragma unroll
             for (int i = 0; i < S::UT; ++i)
-                load_to_lds(xr, s + S::BN * STEP + 16 * (S::threads * i + 64 * wave), off[i] + k0);
+                load_to_lds(xr, s + S::BN * STEP + 16 * (S::threads * i + 64 * wave),
+                            (i == S::UT - 1 ? past : off[i]) + k0);
         };
         // The last stage of a K that is no multiple of STEP holds other bytes
         // behind the row: the units of the weights there count 0.
@@ -323,7 +327,10 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
                 interleave<S>();
             }
         };
+        // the first stage and the folded bias on their way together, and the other
+        // stages behind them
         fill(s0, 0);
+        start();
         fill(s1, 1);
         if constexpr (S::NBUF == 3) fill(s2, 2);
         arrive<(S::NBUF - 1) * kLoads>();
@@ -348,6 +355,7 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
             if (k < nk) stage(s0, s1, k);
         }
     } else {
+        static_assert(S::BT * S::units % S::threads == 0, "whole loads of x");
         vi4 a[S::UN], b[S::UT];
         const int8_t *wrow[S::UN], *xrow[S::UT];
         const int unit = (t % S::units) * 16;
@@ -389,6 +397,7 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
             }
         };
         load(0);
+        start();
         store(s0);
         for (int k = 0; k < nk; k += 2) {
             if (k + 1 < nk) load(k + 1);
@@ -406,15 +415,30 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
     // row, q = 0 .. 3.  A wavefront brings 32 rows at a time through LDS of its
     // own, so that its stores (and the residual's loads) are whole runs of the
     // rows: 128 bytes where FN = 4, instead of 32.
+    vf4 mul[FN][4];
+    if constexpr (!ACC) {
+        const __amdgpu_buffer_rsrc_t mr =
+            __builtin_amdgcn_make_buffer_rsrc((void*)p.mul, (short)0, p.N * 4, 0x00020000);
+#pragma unroll
+        for (int f = 0; f < FN; ++f)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                mul[f][q] = __builtin_bit_cast(
+                    vf4, __builtin_amdgcn_raw_buffer_load_b128(mr, 4 * (n0 + wn + 32 * f + 8 * q + 4 * h),
+                                                               0, 0));
+    }
     arrive<0>();                        // the stages are free, no load under way
-    constexpr int kUnits = ACC ? (FN > 1 ? 8 : 4) : 2 * FN;          // of 16 bytes a row
+    constexpr int kUnits = ACC ? 4 : 2 * FN;          // of 16 bytes a row
     constexpr int kPitch = 16 * kUnits + 16;
     static_assert(32 * kPitch * S::WN * S::WT <= S::bytes && S::bytes >= 16384, "");
     int8_t* own = s0 + 32 * kPitch * wave;
     int8_t* mine = own + (lane & 31) * kPitch + 16 * h;
     // this lane's part of pass i over the rows in memory order
-    constexpr int kRows = 64 / kUnits;
+    constexpr int kRows = 64 / kUnits, kPasses = (32 + kRows - 1) / kRows;
     const int prow = lane / kUnits, punit = lane % kUnits;
+    auto has = [&](int i) __attribute__((always_inline)) {       // a row of the block's 32
+        return 64 % kUnits == 0 || (prow < kRows && prow + i * kRows < 32);
+    };
     const int8_t* part_of = own + prow * kPitch + 16 * punit;
     const int64_t row0 = t0 + wt + prow;
     if constexpr (ACC) {
@@ -431,10 +455,10 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
                 }
                 const int n = n0 + wn + 32 * f + 8 * q0 + 4 * punit;
 #pragma unroll
-                for (int i = 0; i < 32 / kRows; ++i) {
+                for (int i = 0; i < kPasses; ++i) {
                     const vi4 v = *reinterpret_cast<const vi4*>(part_of + i * kRows * kPitch);
                     const int64_t row = row0 + 32 * g + i * kRows;
-                    if (row >= p.T) continue;
+                    if (!has(i) || row >= p.T) continue;
                     int32_t* o = p.acc + row * p.N + n;
                     if (n + 4 <= p.N)
                         __builtin_memcpy(o, &v, 16);
@@ -454,21 +478,22 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
 #pragma unroll
         for (int g = 0; g < FT; ++g) {
             if constexpr (RES) {
-                vi4 r[32 / kRows];
+                vi4 r[kPasses];
 #pragma unroll
-                for (int i = 0; i < 32 / kRows; ++i) {
+                for (int i = 0; i < kPasses; ++i) {
                     const int64_t row = row0 + 32 * g + i * kRows;
                     const int8_t* res = p.residual + row * p.N;
                     r[i] = vi4{0, 0, 0, 0};
-                    if (row >= p.T) continue;
+                    if (!has(i) || row >= p.T) continue;
                     if (whole)
                         __builtin_memcpy(&r[i], res + n, 16);
                     else
                         r[i] = load_end(res, p.N, n);
                 }
 #pragma unroll
-                for (int i = 0; i < 32 / kRows; ++i)
-                    *reinterpret_cast<vi4*>(const_cast<int8_t*>(part_of) + i * kRows * kPitch) = r[i];
+                for (int i = 0; i < kPasses; ++i)
+                    if (has(i))
+                        *reinterpret_cast<vi4*>(const_cast<int8_t*>(part_of) + i * kRows * kPitch) = r[i];
             }
 #pragma unroll
             for (int f = 0; f < FN; ++f) {
@@ -487,11 +512,10 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
                 }
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const vf4 m = *reinterpret_cast<const vf4*>(muls + wn + 32 * f + 8 * q + 4 * h);
                     uint32_t v[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        v[i] = requant<ACT, RES>(acc[f][g][4 * q + i], m[i], byte_of(r[q], i), e, table);
+                        v[i] = requant<ACT, RES>(acc[f][g][4 * q + i], mul[f][q][i], byte_of(r[q], i), e, table);
                     d[q] = pack4(v[0], v[1], v[2], v[3]);
                 }
                 const auto x = __builtin_amdgcn_permlane32_swap(d[0], d[2], false, false);
@@ -499,10 +523,10 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
                 *reinterpret_cast<vi4*>(mine + 32 * f) = vi4{(int)x[0], (int)x[1], (int)z[0], (int)z[1]};
             }
 #pragma unroll
-            for (int i = 0; i < 32 / kRows; ++i) {
+            for (int i = 0; i < kPasses; ++i) {
                 const vi4 v = *reinterpret_cast<const vi4*>(part_of + i * kRows * kPitch);
                 const int64_t row = row0 + 32 * g + i * kRows;
-                if (row >= p.T) continue;
+                if (!has(i) || row >= p.T) continue;
                 int8_t* y = p.y + row * p.N + n;
                 if (whole)
                     __builtin_memcpy(y, &v, 16);
@@ -517,17 +541,24 @@ __global__ __launch_bounds__(S::threads, 2) void linear_tile_kernel(LinearArgs p
 // Launches (tiles: instantiated in linear_tile.hip)
 // ---------------------------------------------------------------------------
 
+// 256 channels x 64 FT rows.  Three stages of 64 inputs and two of 128 do the same
+// (8192 x 8192 x 8192 with FT = 4: 470 us, 2340 TOPS, either way); the first start
+// sooner (788 x 768 x 768 with FT = 3: 9.7 us, 10.4).
 template <int FT>
-using TileW = Shape<4, 2, 2, FT, 128, 2, true>;      // 256 channels x 64 FT rows
-typedef Shape<2, 2, 2, 2, 128, 2, true> Tile128;
-typedef Shape<2, 2, 2, 2, 128, 2, false> Tile128R;
-typedef Shape<2, 2, 1, 1, 128, 3, true> Tile64;
-typedef Shape<2, 2, 1, 1, 128, 2, false> Tile64R;
+using TileW = Shape<4, 2, 2, FT, 64, 3, true, FT == 2 ? 2 : 1>;
+// Smaller tiles: whole 128-byte lines of the rows at a time, which halves the
+// requests to L2 (64 inputs: 1560 TOPS in tiles of 128 x 128 instead of 1870).
+typedef Shape<2, 2, 2, 2, 128, 2, true, 2> Tile128;
+typedef Shape<2, 2, 1, 1, 128, 3, true, 3> Tile64;
+// Rows of any length on bases of any alignment.
+typedef Shape<2, 2, 2, 2, 128, 2, false, 2> Tile128R;
+typedef Shape<2, 2, 1, 1, 128, 2, false, 3> Tile64R;
 
 template <class S>
 void launch_tiles(const LinearArgs& a, hipStream_t stream);
 
-// A few rows of x (linear_rows.hip).
+// Up to 16 FT rows of x (linear_rows.hip).
+template <int FT>
 void launch_rows(const LinearArgs& a, hipStream_t stream);
 
 }  // namespace linear

@@ -79,3 +79,22 @@ def layer(T, K, N, seed, zp_x=0, spread=36.0):
     s_w = (np.exp(g.uniform(-0.7, 0.7, N)) * 1.5 / (s_x * spread * 40 * np.sqrt(K))).astype(np.float32)
     bias = g.normal(0, 0.3, N).astype(np.float32)
     return dict(x=x, w=w, s_w=s_w, bias=bias, s_x=float(s_x), s_y=9.0 / 255, zp_x=zp_x)
+
+
+# Products (T, K, N) for every kernel of the linear layers, by the name of their
+# tile (linear_plan.h): rows and channels that end inside a tile and a unit, one
+# stage of inputs and many, whole and ragged ones.  The first is the smallest.
+KERNELS = ("rows16", "rows32", "tile64", "tile128", "tile256x128", "tile256x192", "tile256x256",
+           "tile256x320", "tile64r", "tile128r")
+PRODUCTS = {
+    "rows16": [(5, 80, 300), (16, 1001, 77)],
+    "rows32": [(17, 80, 300), (32, 1001, 77), (31, 64, 16)],
+    "tile64": [(100, 80, 300), (33, 16, 70), (1000, 400, 1001), (500, 384, 64)],
+    "tile128": [(1130, 80, 1001), (1260, 48, 1001), (2170, 272, 1001), (1000, 400, 2050)],
+    "tile256x128": [(4120, 80, 1001), (1000, 48, 4100), (4120, 272, 1001), (2170, 128, 3000)],
+    "tile256x192": [(3860, 80, 2050), (2690, 48, 3000), (3860, 272, 2050), (3860, 192, 2050)],
+    "tile256x256": [(5420, 80, 2050), (5550, 48, 2050), (5420, 208, 2050), (5420, 256, 2050)],
+    "tile256x320": [(7760, 80, 2050), (7370, 208, 2050), (7370, 400, 2050), (7760, 320, 2050)],
+    "tile64r": [(100, 49, 70), (230, 301, 70), (33, 7, 5), (70, 129, 66)],
+    "tile128r": [(1140, 49, 1001), (1270, 131, 1001), (2050, 301, 1001)],
+}

@@ -2,6 +2,7 @@
 // positions and the heads' way back to rows: each keeps what the C ABI's host
 // code passed it and launches nothing (tests/test_layers_abi.py).
 #include "fqvit_internal.h"
+#include "linear_plan.h"
 
 namespace fqvit {
 
@@ -38,6 +39,8 @@ void fq_test_multipliers(float* out) {
     out[1] = fqvit::g_rope.m_q;
     out[2] = fqvit::g_rope.m_k;
 }
+// The kernel that the last product would take (linear::Kernel).
+int fq_test_linear_kernel(void) { return (int)fqvit::linear::plan(fqvit::g_linear); }
 // N2, N1 of the last requantization; whether the last table had a row per image
 void fq_test_integers(long long* out) {
     out[0] = fqvit::g_heads.r.N2;

@@ -94,6 +94,20 @@ def test_linear_int32_refusals(lib):
         assert call(**{k: None}) == NULL
 
 
+def test_products_of_the_gpu_tests_reach_every_kernel(lib):
+    import layer_cases as R
+    assert set(R.PRODUCTS) == set(R.KERNELS)
+    call = caller(lib, "linear_int32", x=16, T=1, w=16, N=1, K=1, fold=None, out=1)
+    for name, products in R.PRODUCTS.items():
+        for T, K, N in products:
+            assert call(T=T, K=K, N=N) == RAN
+            assert R.KERNELS[lib.fq_test_linear_kernel()] == name, (name, T, K, N)
+    # rows of whole units on other bases take the register path
+    for x, w in ((20, 16), (16, 24)):
+        call(T=100, K=64, N=64, x=x, w=w)
+        assert R.KERNELS[lib.fq_test_linear_kernel()] == "tile64r"
+
+
 def test_rope_refusals(lib):
     call = caller(lib, "rope_table_int16", pos=1, axes=3, T=5, freq=1, axis=1, P=4, table=4)
     assert call() == RAN and call(T=0, pos=None) == EMPTY

@@ -114,6 +114,30 @@ def test_epilogues(fq, act, residual, T, K, N):
         run(fq, R.layer(T, K, N, seed=bits, zp_x=zp), act, residual, zp, bits, seed=T)
 
 
+@pytest.mark.parametrize("name,T,K,N", [(n, *p) for n in R.KERNELS for p in R.PRODUCTS[n]])
+def test_every_kernel(fq, name, T, K, N):
+    """Each kernel on each of its products (that they are its, the CPU test of the
+    same list holds), with a residual on every second."""
+    say("kernel", name, T, K, N)
+    run(fq, R.layer(T, K, N, seed=K, zp_x=-3), "none", K % 32 == 0, 5, seed=N)
+
+
+@pytest.mark.parametrize("name", R.KERNELS)
+@pytest.mark.parametrize("act,residual", [("none", True), ("relu", False), ("relu", True),
+                                          ("table", False), ("table", True), ("int32", False)])
+def test_every_kernel_and_epilogue(fq, name, act, residual):
+    T, K, N = R.PRODUCTS[name][0]
+    say("kernel", name, act, residual)
+    p = R.layer(T, K, N, seed=T)
+    if act == "int32":
+        f = np.random.default_rng(K).integers(-2 ** 30, 2 ** 30, N).astype(np.int32)
+        out, intact = guarded((T, N), dev(f).dtype, 4)
+        fq.linear_int32(dev(p["x"]), dev(p["w"]), dev(f), out=out)
+        assert np.array_equal(host(out), R.sums(p["x"], p["w"], f)) and intact()
+    else:
+        run(fq, p, act, residual, -20, 7, seed=K)
+
+
 @pytest.mark.parametrize("offset", [1, 2, 4, 8, 12, 15])
 @pytest.mark.parametrize("T,K,N", [(1, 64, 64), (9, 48, 20), (150, 128, 132), (260, 100, 64)])
 def test_unaligned_bases(fq, offset, T, K, N):
