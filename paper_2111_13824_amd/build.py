@@ -20,7 +20,7 @@ SOURCES = ["ptf_layernorm.hip", "lis_attention.hip", "lis_inst_lo.hip", "lis_ins
            "linear.hip", "linear_rows.hip", "linear_tile.hip:FQ_TILE_W=2",
            "linear_tile.hip:FQ_TILE_W=3", "linear_tile.hip:FQ_TILE_W=4",
            "linear_tile.hip:FQ_TILE_W=5", "linear_tile.hip:FQ_TILE_128",
-           "linear_tile.hip:FQ_TILE_64", "heads.hip",
+           "linear_tile.hip:FQ_TILE_64", "linear_tile.hip:FQ_TILE_256R", "heads.hip",
            "fqvit_abi.cpp"]     # "file:MACRO": compiled with -DMACRO
 OBJDIR = os.path.join(HERE, "_build")
 

@@ -51,6 +51,7 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
         case kTileW5: launch_tiles<TileW<5>>(a, stream); break;
         case kTile64R: launch_tiles<Tile64R>(a, stream); break;
         case kTile128R: launch_tiles<Tile128R>(a, stream); break;
+        case kTile256R: launch_tiles<Tile256R>(a, stream); break;
     }
     return hipGetLastError();
 }

@@ -15,8 +15,9 @@ enum Kernel {
     kTileW3,
     kTileW4,
     kTileW5,
-    kTile64R,       // 64 x 64 and 128 x 128 with the loads through registers
+    kTile64R,       // 64 x 64, 128 x 128, 256 x 256 with the loads through registers
     kTile128R,
+    kTile256R,
 };
 
 // Products of so few rows take the kernel that shares the inputs out among the
@@ -43,14 +44,24 @@ constexpr Cost kCosts[] = {
     {256, 256, 1, 1.0f, 3.3f, 8.5e-3f},  {256, 320, 1, 1.0f, 5.2f, 9.6e-3f},
 };
 
-inline int cheapest(int64_t T, int32_t N, int32_t K, int shapes) {
+// The same for the loads through registers (99 products, K 47 .. 4091, N 101 .. 4097):
+// 9232 x 1021 x 4097 takes 68 us in tiles of 256 x 256, 86 in 128 x 128 and 137 in 64 x
+// 64; 788 x 1021 x 1021 7.8 in 64 x 64, 14.9 in 128 x 128 and 24.9 in 256 x 256.
+constexpr Cost kCostsR[] = {
+    {64, 64, 3, 0.51f, 2.1f, 14.1e-3f},
+    {128, 128, 2, 0.92f, 7.6f, 9.1e-3f},
+    {256, 256, 1, 1.0f, 7.3f, 13.0e-3f},
+};
+
+template <int shapes>
+int cheapest(const LinearArgs& a, const Cost (&costs)[shapes]) {
     int best = 0;
     float least = 0;
     for (int i = 0; i < shapes; ++i) {
-        const Cost& c = kCosts[i];
-        const int64_t tiles = ((N + c.bn - 1) / c.bn) * ((T + c.bt - 1) / c.bt);
+        const Cost& c = costs[i];
+        const int64_t tiles = ((a.N + c.bn - 1) / c.bn) * ((a.T + c.bt - 1) / c.bt);
         const float share = (float)((tiles + 255) / 256) / (float)c.per;
-        const float cost = (share > c.few ? share : c.few) * (c.fixed + c.input * (float)K);
+        const float cost = (share > c.few ? share : c.few) * (c.fixed + c.input * (float)a.K);
         if (i == 0 || cost < least) {
             best = i;
             least = cost;
@@ -66,8 +77,8 @@ inline Kernel plan(const LinearArgs& a) {
     if (a.T <= kFewRows) return kRows32;
     const bool units = a.K % 16 == 0 &&
                        ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15) == 0;
-    return units ? (Kernel)(kTile64 + cheapest(a.T, a.N, a.K, 6))
-                 : (Kernel)(kTile64R + cheapest(a.T, a.N, a.K, 2));
+    return units ? (Kernel)(kTile64 + cheapest(a, kCosts))
+                 : (Kernel)(kTile64R + cheapest(a, kCostsR));
 }
 
 }  // namespace linear

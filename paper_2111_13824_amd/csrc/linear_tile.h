@@ -553,6 +553,7 @@ typedef Shape<2, 2, 1, 1, 128, 3, true, 3> Tile64;
 // Rows of any length on bases of any alignment.
 typedef Shape<2, 2, 2, 2, 128, 2, false, 2> Tile128R;
 typedef Shape<2, 2, 1, 1, 128, 2, false, 3> Tile64R;
+typedef Shape<4, 2, 2, 4, 64, 2, false, 1> Tile256R;
 
 template <class S>
 void launch_tiles(const LinearArgs& a, hipStream_t stream);

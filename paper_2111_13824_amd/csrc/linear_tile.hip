@@ -31,6 +31,8 @@ void launch_tiles(const LinearArgs& a, hipStream_t stream) {
 
 #if defined(FQ_TILE_W)
 template void launch_tiles<TileW<FQ_TILE_W>>(const LinearArgs&, hipStream_t);
+#elif defined(FQ_TILE_256R)
+template void launch_tiles<Tile256R>(const LinearArgs&, hipStream_t);
 #elif defined(FQ_TILE_128)
 template void launch_tiles<Tile128>(const LinearArgs&, hipStream_t);
 template void launch_tiles<Tile128R>(const LinearArgs&, hipStream_t);

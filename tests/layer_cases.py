@@ -85,7 +85,7 @@ def layer(T, K, N, seed, zp_x=0, spread=36.0):
 # tile (linear_plan.h): rows and channels that end inside a tile and a unit, one
 # stage of inputs and many, whole and ragged ones.  The first is the smallest.
 KERNELS = ("rows16", "rows32", "tile64", "tile128", "tile256x128", "tile256x192", "tile256x256",
-           "tile256x320", "tile64r", "tile128r")
+           "tile256x320", "tile64r", "tile128r", "tile256r")
 PRODUCTS = {
     "rows16": [(5, 80, 300), (16, 1001, 77)],
     "rows32": [(17, 80, 300), (32, 1001, 77), (31, 64, 16)],
@@ -96,5 +96,6 @@ PRODUCTS = {
     "tile256x256": [(5420, 80, 2050), (5550, 48, 2050), (5420, 208, 2050), (5420, 256, 2050)],
     "tile256x320": [(7760, 80, 2050), (7370, 208, 2050), (7370, 400, 2050), (7760, 320, 2050)],
     "tile64r": [(100, 49, 70), (230, 301, 70), (33, 7, 5), (70, 129, 66)],
-    "tile128r": [(1140, 49, 1001), (1270, 131, 1001), (2050, 301, 1001)],
+    "tile128r": [(2960, 131, 2050), (2050, 301, 2050), (4130, 301, 1001)],
+    "tile256r": [(4000, 49, 2050), (3870, 131, 2050), (4130, 65, 2050)],
 }
