@@ -175,41 +175,33 @@ def _invoke(name: str, args, keep, prepare: bool, result, device: Optional[int] 
     """Run the entry point now, or return it prepared for repeated calls."""
     if prepare:
         return Prepared(name, args, keep, device)
-    _check(name, _enter(getattr(lib(), name), args, device))
+    st = _enter(getattr(_lib or lib(), name), args, device)
+    if st != FQ_OK:
+        raise FqError(name, st)
     return result
 
 
-def _device_of(t, name: str) -> int:
-    """The index of the device that tensor `t` lies on."""
-    try:
-        device = t.get_device()
-    except AttributeError:
-        raise TypeError(f"{name} must be a torch.Tensor") from None
-    if device < 0:
-        raise ValueError(f"{name} must be a device tensor")
-    return device
-
-
-def _arg(t, dtype, shape, device: int, name: str):
-    """The address of tensor `t` (None for None), which has to be contiguous, of
-    this dtype and shape, on this device."""
-    if t is None:
-        return None
-    try:
-        if (t.dtype is dtype and t.shape == shape and t.get_device() == device
-                and t.is_contiguous()):
-            return t.data_ptr()
-    except AttributeError:
-        raise TypeError(f"{name} must be a torch.Tensor") from None
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if t.get_device() < 0:
-        raise ValueError(f"{name} must be a device tensor")
-    raise ValueError(f"{name} must be on device {device}, got {t.device}")
+def _refuse(device: int, *specs):
+    """Raises for the first of (name, tensor, dtype, shape) that does not fit: a
+    contiguous tensor of that dtype and shape (None where the argument may be
+    left out: the spec is then not given), all on one device.  The functions
+    below ask this only where one expression over all their tensors has failed:
+    a call of a helper for each tensor would take a seventh of a short call."""
+    for name, t, dtype, shape in specs:
+        if not hasattr(t, "is_contiguous"):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    for name, t, _, _ in specs:
+        if t.get_device() < 0:
+            raise ValueError(f"{name} must be a device tensor")
+        if t.get_device() != device:
+            raise ValueError(f"{name} must be on device {device}, got {t.device}")
+    raise ValueError("arguments do not fit together")
 
 
 def _dims(t, n: int, name: str):
@@ -218,6 +210,14 @@ def _dims(t, n: int, name: str):
     if len(shape) != n:
         raise ValueError(f"{name} must have {n} dimensions, got {len(shape)}")
     return shape
+
+
+def _raw_stream(stream, device: int) -> int:
+    """Raw hipStream_t: the given torch stream, else the device's current one."""
+    if stream is not None:
+        return stream.cuda_stream
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def ptf_layernorm_int8(x_q, zp_in: int, alpha, K: int, gamma, beta, s_out: float, zp_out: int,
@@ -433,15 +433,21 @@ def linear_fold_int8(w, s_w, s_x: float, s_y: float = 1.0, zp_x: int = 0, bias=N
     an activation table follows).  Once for a layer."""
     import torch
     N, K = _dims(w, 2, "w")
-    dev = _device_of(w, "w")
+    dev = w.get_device()
     if fold is None:
         fold = torch.empty(N, dtype=torch.int32, device=w.device)
     if mul is None:
         mul = torch.empty(N, dtype=torch.float32, device=w.device)
-    args = (_arg(w, torch.int8, (N, K), dev, "w"), N, K, _arg(s_w, torch.float32, (N,), dev, "s_w"),
-            _arg(bias, torch.float32, (N,), dev, "bias"), zp_x, s_x, s_y,
-            _arg(fold, torch.int32, (N,), dev, "fold"), _arg(mul, torch.float32, (N,), dev, "mul"),
-            _stream(stream, w))
+    specs = [("w", w, torch.int8, (N, K)), ("s_w", s_w, torch.float32, (N,)),
+             ("fold", fold, torch.int32, (N,)), ("mul", mul, torch.float32, (N,))]
+    if bias is not None:
+        specs.append(("bias", bias, torch.float32, (N,)))
+    for _, t, dtype, shape in specs:
+        if not (hasattr(t, "is_contiguous") and t.dtype is dtype and t.shape == shape
+                and t.is_contiguous() and t.get_device() == dev >= 0):
+            _refuse(dev, *specs)
+    args = (w.data_ptr(), N, K, s_w.data_ptr(), None if bias is None else bias.data_ptr(), zp_x, s_x,
+            s_y, fold.data_ptr(), mul.data_ptr(), _raw_stream(stream, dev))
     return _invoke("linear_fold_int8", args, (w, s_w, bias, fold, mul), prepare, (fold, mul), dev)
 
 
@@ -454,10 +460,10 @@ def linear_int8(x, w, fold, mul, zp_y: int = 0, bits: int = 8, relu: bool = Fals
     zero point zp_r and mul_r = s_r / s_y is added after the activation.  y may
     be the residual."""
     import torch
-    i8, f32 = torch.int8, torch.float32
+    i8, i32, f32 = torch.int8, torch.int32, torch.float32
     T, K = _dims(x, 2, "x")
     N = w.shape[0]
-    dev = _device_of(x, "x")
+    dev = x.get_device()
     act, bits_t, size = ACT_NONE, 0, 0
     if table is not None:
         if relu:
@@ -466,30 +472,64 @@ def linear_int8(x, w, fold, mul, zp_y: int = 0, bits: int = 8, relu: bool = Fals
         bits_t = size.bit_length() - 1
         if size != 1 << bits_t:
             raise ValueError("table must hold a power of two of values")
-        zp_t = size >> 1 if zp_t is None else zp_t
+        if zp_t is None:
+            zp_t = size >> 1
     elif relu:
         act = ACT_RELU
-    px = _arg(x, i8, (T, K), dev, "x")
     if y is None:
         y = x.new_empty((T, N))
-    args = (px, T, _arg(w, i8, (N, K), dev, "w"), N, K, _arg(fold, torch.int32, (N,), dev, "fold"),
-            _arg(mul, f32, (N,), dev, "mul"), act, _arg(table, f32, (size,), dev, "table"), bits_t,
-            zp_t or 0, _arg(residual, i8, (T, N), dev, "residual"), zp_r, mul_r, zp_y, bits,
-            _arg(y, i8, (T, N), dev, "y"), _stream(stream, x))
+    try:
+        fits = (x.dtype is i8 and x.is_contiguous() and dev >= 0
+                and w.dtype is i8 and w.shape == (N, K) and w.is_contiguous()
+                and w.get_device() == dev
+                and mul.dtype is f32 and mul.shape == (N,) and mul.is_contiguous()
+                and mul.get_device() == dev
+                and y.dtype is i8 and y.shape == (T, N) and y.is_contiguous()
+                and y.get_device() == dev
+                and (fold is None or fold.dtype is i32 and fold.shape == (N,)
+                     and fold.is_contiguous() and fold.get_device() == dev)
+                and (table is None or table.dtype is f32 and table.shape == (size,)
+                     and table.is_contiguous() and table.get_device() == dev)
+                and (residual is None or residual.dtype is i8 and residual.shape == (T, N)
+                     and residual.is_contiguous() and residual.get_device() == dev))
+    except AttributeError:
+        fits = False
+    if not fits:
+        _refuse(dev, ("x", x, i8, (T, K)), ("w", w, i8, (N, K)), ("mul", mul, f32, (N,)),
+                *[s for s in (("fold", fold, i32, (N,)), ("table", table, f32, (size,)),
+                              ("residual", residual, i8, (T, N))) if s[1] is not None],
+                ("y", y, i8, (T, N)))
+    args = (x.data_ptr(), T, w.data_ptr(), N, K, None if fold is None else fold.data_ptr(),
+            mul.data_ptr(), act, None if table is None else table.data_ptr(), bits_t, zp_t or 0,
+            None if residual is None else residual.data_ptr(), zp_r, mul_r, zp_y, bits, y.data_ptr(),
+            _raw_stream(stream, dev))
     return _invoke("linear_int8", args, (x, w, fold, mul, table, residual, y), prepare, y, dev)
 
 
 def linear_int32(x, w, fold=None, out=None, stream=None, prepare: bool = False):
     """The linear layer's accumulators: int32 [T, N] = x w^T + fold."""
     import torch
+    i8, i32 = torch.int8, torch.int32
     T, K = _dims(x, 2, "x")
     N = w.shape[0]
-    dev = _device_of(x, "x")
+    dev = x.get_device()
     if out is None:
-        out = torch.empty((T, N), dtype=torch.int32, device=x.device)
-    args = (_arg(x, torch.int8, (T, K), dev, "x"), T, _arg(w, torch.int8, (N, K), dev, "w"), N, K,
-            _arg(fold, torch.int32, (N,), dev, "fold"), _arg(out, torch.int32, (T, N), dev, "out"),
-            _stream(stream, x))
+        out = torch.empty((T, N), dtype=i32, device=x.device)
+    try:
+        fits = (x.dtype is i8 and x.is_contiguous() and dev >= 0
+                and w.dtype is i8 and w.shape == (N, K) and w.is_contiguous()
+                and w.get_device() == dev
+                and out.dtype is i32 and out.shape == (T, N) and out.is_contiguous()
+                and out.get_device() == dev
+                and (fold is None or fold.dtype is i32 and fold.shape == (N,)
+                     and fold.is_contiguous() and fold.get_device() == dev))
+    except AttributeError:
+        fits = False
+    if not fits:
+        _refuse(dev, ("x", x, i8, (T, K)), ("w", w, i8, (N, K)),
+                *([] if fold is None else [("fold", fold, i32, (N,))]), ("out", out, i32, (T, N)))
+    args = (x.data_ptr(), T, w.data_ptr(), N, K, None if fold is None else fold.data_ptr(),
+            out.data_ptr(), _raw_stream(stream, dev))
     return _invoke("linear_int32", args, (x, w, fold, out), prepare, out, dev)
 
 
@@ -514,14 +554,26 @@ def rope_table_int16(positions, freq, axis, table=None, stream=None, prepare: bo
     """cos and sin of positions int32 [axes, T] times freq float64 [P], pair p
     along axis[p] (uint8 [P]), in steps of 2^-14: int16 [T, P, 2]."""
     import torch
+    i32, f64, u8, i16 = torch.int32, torch.float64, torch.uint8, torch.int16
     axes, T = _dims(positions, 2, "positions")
     P, = _dims(freq, 1, "freq")
-    dev = _device_of(positions, "positions")
+    dev = positions.get_device()
     if table is None:
-        table = torch.empty((T, P, 2), dtype=torch.int16, device=positions.device)
-    args = (_arg(positions, torch.int32, (axes, T), dev, "positions"), axes, T,
-            _arg(freq, torch.float64, (P,), dev, "freq"), _arg(axis, torch.uint8, (P,), dev, "axis"),
-            P, _arg(table, torch.int16, (T, P, 2), dev, "table"), _stream(stream, positions))
+        table = torch.empty((T, P, 2), dtype=i16, device=positions.device)
+    try:
+        fits = (positions.dtype is i32 and positions.is_contiguous() and dev >= 0
+                and freq.dtype is f64 and freq.is_contiguous() and freq.get_device() == dev
+                and axis.dtype is u8 and axis.shape == (P,) and axis.is_contiguous()
+                and axis.get_device() == dev
+                and table.dtype is i16 and table.shape == (T, P, 2) and table.is_contiguous()
+                and table.get_device() == dev)
+    except AttributeError:
+        fits = False
+    if not fits:
+        _refuse(dev, ("positions", positions, i32, (axes, T)), ("freq", freq, f64, (P,)),
+                ("axis", axis, u8, (P,)), ("table", table, i16, (T, P, 2)))
+    args = (positions.data_ptr(), axes, T, freq.data_ptr(), axis.data_ptr(), P, table.data_ptr(),
+            _raw_stream(stream, dev))
     return _invoke("rope_table_int16", args, (positions, freq, axis, table), prepare, table, dev)
 
 
@@ -532,25 +584,37 @@ def rope_qkv_int8(qkv, table, Hq: int, Hkv: int, s_x: float, s_q: float, s_k: fl
     heads, queries and keys rotated by the table (int16 [L or B L, P, 2]; None:
     no rotation) and requantized: (q [B, Hq, L, d], k and v [B, Hkv, L, d])."""
     import torch
-    i8 = torch.int8
+    i8, i16 = torch.int8, torch.int16
     B, L, row = _dims(qkv, 3, "qkv")
     heads = Hq + 2 * Hkv
     if Hq < 1 or Hkv < 1 or row % heads:
         raise ValueError("qkv must be [B, L, (Hq + 2 Hkv) d]")
     d = row // heads
-    dev = _device_of(qkv, "qkv")
+    dev = qkv.get_device()
     rows, P = (0, 0) if table is None else _dims(table, 3, "table")[:2]
     sq, sk = (B, Hq, L, d), (B, Hkv, L, d)
-    px = _arg(qkv, i8, (B, L, row), dev, "qkv")
     if q is None:
         q = qkv.new_empty(sq)
     if k is None:
         k = qkv.new_empty(sk)
     if v is None:
         v = qkv.new_empty(sk)
-    args = (px, B, L, Hq, Hkv, d, s_x, zp_x, _arg(table, torch.int16, (rows, P, 2), dev, "table"),
-            rows, P, 1 if interleaved else 0, s_q, zp_q, s_k, zp_k, bits, _arg(q, i8, sq, dev, "q"),
-            _arg(k, i8, sk, dev, "k"), _arg(v, i8, sk, dev, "v"), _stream(stream, qkv))
+    try:
+        fits = (qkv.dtype is i8 and qkv.is_contiguous() and dev >= 0
+                and (table is None or table.dtype is i16 and table.shape == (rows, P, 2)
+                     and table.is_contiguous() and table.get_device() == dev)
+                and q.dtype is i8 and q.shape == sq and q.is_contiguous() and q.get_device() == dev
+                and k.dtype is i8 and k.shape == sk and k.is_contiguous() and k.get_device() == dev
+                and v.dtype is i8 and v.shape == sk and v.is_contiguous() and v.get_device() == dev)
+    except AttributeError:
+        fits = False
+    if not fits:
+        _refuse(dev, ("qkv", qkv, i8, (B, L, row)),
+                *([] if table is None else [("table", table, i16, (rows, P, 2))]),
+                ("q", q, i8, sq), ("k", k, i8, sk), ("v", v, i8, sk))
+    args = (qkv.data_ptr(), B, L, Hq, Hkv, d, s_x, zp_x, None if table is None else table.data_ptr(),
+            rows, P, 1 if interleaved else 0, s_q, zp_q, s_k, zp_k, bits, q.data_ptr(), k.data_ptr(),
+            v.data_ptr(), _raw_stream(stream, dev))
     return _invoke("rope_qkv_int8", args, (qkv, table, q, k, v), prepare, (q, k, v), dev)
 
 
@@ -559,11 +623,19 @@ def requant_heads_int8(q, s_in: float, s_out: float, zp_out: int, bits: int = 8,
     """Dyadic requantization of an attention result int32 [B, H, L, d] with its
     heads brought back to rows: int8 [B, L, H d]."""
     import torch
+    i8, i32 = torch.int8, torch.int32
     B, H, L, d = _dims(q, 4, "q")
-    dev = _device_of(q, "q")
-    shape = (B, L, H * d)
+    dev = q.get_device()
     if y is None:
-        y = torch.empty(shape, dtype=torch.int8, device=q.device)
-    args = (_arg(q, torch.int32, (B, H, L, d), dev, "q"), B, H, L, d, s_in, s_out, zp_out, bits,
-            _arg(y, torch.int8, shape, dev, "y"), _stream(stream, q))
+        y = torch.empty((B, L, H * d), dtype=i8, device=q.device)
+    try:
+        fits = (q.dtype is i32 and q.is_contiguous() and dev >= 0
+                and y.dtype is i8 and y.shape == (B, L, H * d) and y.is_contiguous()
+                and y.get_device() == dev)
+    except AttributeError:
+        fits = False
+    if not fits:
+        _refuse(dev, ("q", q, i32, (B, H, L, d)), ("y", y, i8, (B, L, H * d)))
+    args = (q.data_ptr(), B, H, L, d, s_in, s_out, zp_out, bits, y.data_ptr(),
+            _raw_stream(stream, dev))
     return _invoke("requant_heads_int8", args, (q, y), prepare, y, dev)
