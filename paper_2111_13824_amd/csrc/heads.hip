@@ -2,7 +2,7 @@
 // heads back to rows, for gfx950.  Both move each byte once and are bound by
 // memory: what counts is that rows are read and written in whole lines with many
 // loads under way.  On ViT-L/16 at batch 16 (9232 rows of 48 heads of 64, 57 MB) the
-// rotation takes 12.9 us, 4.4 TB/s; on ViT-B/16 at batch 64 the way back to rows
+// rotation takes 11.9 us, 4.8 TB/s; on ViT-B/16 at batch 64 the way back to rows
 // (48 MB) 8.6 to 9.1 us, 5.5 TB/s; a large copy reaches 5.1.
 #include <algorithm>
 
@@ -52,6 +52,17 @@ template <int V>
 struct Bytes {
     uint32_t w[V / 4];
 };
+
+// V bytes to an address of their alignment, past L2: the next kernel reads rows of
+// many megabytes from elsewhere by then (9232 rows of 48 heads of 64: 13.3 -> 11.9 us).
+template <int V>
+__device__ __forceinline__ void store_bytes(int8_t* at, const Bytes<V>& b) {
+    typedef uint32_t words __attribute__((ext_vector_type(V / 4)));
+    if constexpr (V == 4)
+        __builtin_nontemporal_store(b.w[0], reinterpret_cast<uint32_t*>(at));
+    else
+        __builtin_nontemporal_store(__builtin_bit_cast(words, b), reinterpret_cast<words*>(at));
+}
 
 // V bytes at any address.
 template <int V>
@@ -150,7 +161,7 @@ __global__ __launch_bounds__(kBlock) void rope_qkv_kernel(RopeArgs p, int64_t ti
 
     auto one = [&](B x, int h) __attribute__((always_inline)) {
         if (h >= p.Hq + p.Hkv) {
-            if (live) *reinterpret_cast<B*>(v + (h - p.Hq - p.Hkv) * step) = x;
+            if (live) store_bytes<V>(v + (h - p.Hq - p.Hkv) * step, x);
             return;
         }
         const bool is_q = h < p.Hq;
@@ -182,7 +193,7 @@ __global__ __launch_bounds__(kBlock) void rope_qkv_kernel(RopeArgs p, int64_t ti
             out.w[i] = __builtin_amdgcn_perm(r[1], r[0], 0x0c0c0400u) |
                        __builtin_amdgcn_perm(r[3], r[2], 0x04000c0cu);
         }
-        if (live) *reinterpret_cast<B*>(is_q ? q + h * step : kk + (h - p.Hq) * step) = out;
+        if (live) store_bytes<V>(is_q ? q + h * step : kk + (h - p.Hq) * step, out);
     };
 
     constexpr int kAhead = 4;
