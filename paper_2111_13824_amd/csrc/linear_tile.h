@@ -116,12 +116,10 @@ struct Shape {
     static constexpr int waves = PER * WN * WT / 4;       // a SIMD: PER workgroups a CU
     static constexpr int BN = 32 * WN * FN, BT = 32 * WT * FT;
     static constexpr int units = STEP / 16;                               // of a row
-    // Loads of a thread a stage; where they come out uneven, a stage has room for
-    // the rows behind the tile that the last ones are for.
-    static constexpr int UN = (BN * units + threads - 1) / threads;
-    static constexpr int UT = (BT * units + threads - 1) / threads;
-    static_assert(BN * units % threads == 0, "whole loads of the weights");
-    static constexpr int bytes = BN * STEP + UT * threads * 16;
+    // loads of a thread a stage
+    static constexpr int UN = BN * units / threads, UT = BT * units / threads;
+    static_assert(BN * units % threads == 0 && BT * units % threads == 0, "whole loads");
+    static constexpr int bytes = (BN + BT) * STEP;
     static constexpr int slice = STEP == 128 ? 1 : 2;
 
     // The place in a stage of a row's unit.
@@ -283,10 +281,9 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
         // arrive() counts stay the same
         constexpr unsigned kNone = 0x70000000u;
         constexpr int U = S::UN > S::UT ? S::UN : S::UT;
-        unsigned off[U], past = kNone;      // past: of the last loads of x, if uneven
+        unsigned off[U];
 #pragma unroll
         for (int i = 0; i < U; ++i) off[i] = S::fill_row(t, i) * K + S::fill_unit(t, i) * 16;
-        if (S::fill_row(t, S::UT - 1) < S::BT) past = off[S::UT - 1];
         auto fill = [&](int8_t* s, int k) __attribute__((always_inline)) {
             const unsigned k0 = k < nk ? k * STEP : kNone;
 #pragma unroll
@@ -294,8 +291,7 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
                 load_to_lds(wr, s + 16 * (S::threads * i + 64 * wave), off[i] + k0);
 #pragma unroll
             for (int i = 0; i < S::UT; ++i)
-                load_to_lds(xr, s + S::BN * STEP + 16 * (S::threads * i + 64 * wave),
-                            (i == S::UT - 1 ? past : off[i]) + k0);
+                load_to_lds(xr, s + S::BN * STEP + 16 * (S::threads * i + 64 * wave), off[i] + k0);
         };
         // The last stage of a K that is no multiple of STEP holds other bytes
         // behind the row: the units of the weights there count 0.
@@ -356,7 +352,6 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
             if (k < nk) stage(s0, s1, k);
         }
     } else {
-        static_assert(S::BT * S::units % S::threads == 0, "whole loads of x");
         vi4 a[S::UN], b[S::UT];
         const int8_t *wrow[S::UN], *xrow[S::UT];
         const int unit = (t % S::units) * 16;
@@ -546,11 +541,13 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
 // Launches (tiles: instantiated in linear_tile.hip)
 // ---------------------------------------------------------------------------
 
-// 256 channels x 64 FT rows.  Three stages of 64 inputs and two of 128 do the same
-// (8192 x 8192 x 8192 with FT = 4: 470 us, 2340 TOPS, either way); the first start
-// sooner (788 x 768 x 768 with FT = 3: 9.7 us, 10.4).
+// 256 channels x 64 FT rows.  Two stages of 128 inputs, whole 128-byte lines of the
+// rows, or three of 64, half lines: 12608 x 768 x 2304 takes 30.2 us with the first and
+// 32.4 with the second (inputs that were not read just before), the longer
+// products 9232 x 4096 x 1024 and 9232 x 1024 x 4096 the same with both.  The smallest
+// has room for two workgroups on a CU with the second.
 template <int FT>
-using TileW = Shape<4, 2, 2, FT, 64, 3, true, FT == 2 ? 2 : 1>;
+using TileW = Shape<4, 2, 2, FT, (FT > 2 ? 128 : 64), (FT > 2 ? 2 : 3), true, (FT > 2 ? 1 : 2)>;
 // Smaller tiles: whole 128-byte lines of the rows at a time, which halves the
 // requests to L2 (64 inputs: 1560 TOPS in tiles of 128 x 128 instead of 1870).
 typedef Shape<2, 2, 2, 2, 128, 2, true, 2> Tile128;
