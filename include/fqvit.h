@@ -354,8 +354,9 @@ fq_status linear_fold_int8(const int8_t* w, int32_t N, int32_t K, const float* s
  *   zp_y, bits  the output's zero point (container form) and grid, b in [2, 8].
  *   y      [T, N] int8 container (out).  It may be the residual itself; it
  *          overlaps no other argument.
- * T >= 0, N in [1, 2^20], K in [1, 32768].  Bases of any alignment; rows of
- * whole 16-byte units on 16-byte aligned bases take the fast path.
+ * T >= 0, N in [1, 2^20], K in [1, 32768], fewer than 2^24 tiles of 64 x 64
+ * outputs.  Bases of any alignment; rows of whole 16-byte units on 16-byte aligned
+ * bases take the fast path.
  *
  * With acc = sum_k x[t,k] w[n,k] + fold[n] exact in int32, RN = rounding to the
  * nearest binary32 and rint = to the nearest integer (ties to even in both), of
@@ -374,8 +375,8 @@ fq_status linear_fold_int8(const int8_t* w, int32_t N, int32_t K, const float* s
  * function's values in steps of the output, f(s_t (u - zp_t)) / s_y; then mul
  * was folded with the table's step s_t in the place of s_y.
  * Errors: FQ_ERR_NULL (x, w, mul, y; table with FQ_ACT_TABLE), FQ_ERR_SHAPE
- * (T, N or K, or more tiles than a grid holds), FQ_ERR_PARAM (act, table_bits,
- * zp_t, zero points, mul_r, bits).
+ * (T, N, K or the tiles), FQ_ERR_PARAM (act, table_bits, zp_t, zero points,
+ * mul_r, bits).
  */
 fq_status linear_int8(const int8_t* x, int64_t T, const int8_t* w, int32_t N, int32_t K,
                       const int32_t* fold, const float* mul, int32_t act, const float* table,
@@ -417,12 +418,12 @@ fq_status fq_activation_table(int32_t kind, float s_t, int32_t zp_t, int32_t tab
  * an entry may be the other neighbour only where 2^14 cos t lies that close to
  * the middle of two integers.  Position 0 gives (2^14, 0): no turn at all.
  *
- *   positions  [axes, T] int32, axes in [1, 8].
+ *   positions  [axes, T] int32, axes in [1, 8], T in [0, 2^25].
  *   freq   [P] double (finite), P in [1, 128]; axis [P] uint8 (values at or
  *          above `axes` are taken as axes - 1).
  *   table  [T, P, 2] int16 (out), 4-byte aligned.
- * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (T < 0 or above 2^31 - 1, axes, P),
- * FQ_ERR_PARAM (table not aligned).
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (T, axes, P), FQ_ERR_PARAM (table not
+ * aligned).
  */
 fq_status rope_table_int16(const int32_t* positions, int32_t axes, int64_t T, const double* freq,
                            const uint8_t* axis, int32_t P, int16_t* table, void* stream);
@@ -432,8 +433,8 @@ fq_status rope_table_int16(const int32_t* positions, int32_t axes, int64_t T, co
  * and requantized, as lis_attention_qk takes them.
  *
  *   qkv    [B, L, (Hq + 2 Hkv) d] int8 with scale s_x and zero point zp_x: the
- *          query heads, the key heads, the value heads.  Hq, Hkv in [1, 1024],
- *          d in [1, 256].
+ *          query heads, the key heads, the value heads.  B L in [0, 2^25], Hq, Hkv
+ *          in [1, 1024], d in [1, 256].
  *   table  [table_rows, P, 2] int16, 4-byte aligned, as rope_table_int16 writes
  *          it; table_rows is L (one grid for every b) or B L.  P in [0, d / 2]
  *          pairs turn, the d - 2 P values after them do not.  P = 0: table may
@@ -442,7 +443,8 @@ fq_status rope_table_int16(const int32_t* positions, int32_t axes, int64_t T, co
  *   q      [B, Hq, L, d] int8 (out), scale s_q, zero point zp_q (container of
  *          the b-bit grid); k [B, Hkv, L, d] (out), s_k, zp_k; v [B, Hkv, L, d]
  *          (out), the values as they are.  With Hq = r Hkv, q read as
- *          [B Hkv, r L, d] are the queries of each key head.
+ *          [B Hkv, r L, d] are the queries of each key head.  The outputs overlap
+ *          no other argument.
  * With (f, g) a pair less zp_x and (c, s) its table entry, the turned pair is
  * (f c - g s, f s + g c), exact in 32 bits for |c|, |s| <= 2^14; a value that
  * does not turn counts 2^14 times itself less zp_x.  Each, a, becomes
@@ -460,7 +462,7 @@ fq_status rope_qkv_int8(const int8_t* qkv, int64_t B, int32_t L, int32_t Hq, int
  * requant_dyadic_int8 of an attention result, with its heads brought back to
  * rows: q [B, H, L, d] int32 (lis_attention_qk's out) -> y [B, L, H d] int8, as
  * the projection's linear layer reads it.  The same dyadic multiplier and
- * rounding; H in [1, 1024], d in [1, 256].
+ * rounding; B L in [0, 2^25], H in [1, 1024], d in [1, 256].
  * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (B or L < 0, H, d), FQ_ERR_PARAM (bits, a
  * scale or zp_out out of range).
  */

@@ -109,10 +109,17 @@ float multiplier(double num, double den) {
 bool positive(float s) { return s > 0.0f && std::isfinite(s); }
 bool int8_zp(int32_t zp) { return zp >= -128 && zp <= 127; }
 
-// Sizes of a linear product.  The smallest tile is 16 x 16.
+// Sizes of a linear product.  A launch has fewer than 2^32 threads: the smallest
+// tiles, 64 x 64, have 256 each.
 bool linear_sizes(int64_t T, int32_t N, int32_t K) {
     if (T < 0 || T > ((int64_t)1 << 40) || N < 1 || N > kMaxN || K < 1 || K > kMaxK) return false;
-    return ((T + 15) / 16) <= (int64_t)0x7FFFFFFF / ((N + 15) / 16);
+    return (T + 63) / 64 * ((N + 63) / 64) < ((int64_t)1 << 24);
+}
+
+// Tokens of the rotation and of the heads' way back: a wavefront holds one or more.
+constexpr int64_t kMaxTokens = (int64_t)1 << 25;
+bool token_count(int64_t B, int32_t L) {
+    return B >= 0 && L >= 0 && (L == 0 || B <= kMaxTokens / L);
 }
 
 // The launch, where this build has its kernels.
@@ -459,7 +466,7 @@ fq_status fq_activation_table(int32_t kind, float s_t, int32_t zp_t, int32_t tab
 fq_status rope_table_int16(const int32_t* positions, int32_t axes, int64_t T, const double* freq,
                            const uint8_t* axis, int32_t P, int16_t* table, void* stream) {
     ConsumeEvents consume;
-    if (T < 0 || T > 0x7FFFFFFF || axes < 1 || axes > 8 || P < 1 || P > kMaxD / 2)
+    if (T < 0 || T > kMaxTokens || axes < 1 || axes > 8 || P < 1 || P > kMaxD / 2)
         return FQ_ERR_SHAPE;
     if (T == 0) return FQ_OK;
     if (!positions || !freq || !axis || !table) return FQ_ERR_NULL;
@@ -473,8 +480,8 @@ fq_status rope_qkv_int8(const int8_t* qkv, int64_t B, int32_t L, int32_t Hq, int
                         int32_t interleaved, float s_q, int32_t zp_q, float s_k, int32_t zp_k,
                         int32_t bits, int8_t* q, int8_t* k, int8_t* v, void* stream) {
     ConsumeEvents consume;
-    if (B < 0 || L < 0 || Hq < 1 || Hq > kMaxHeads || Hkv < 1 || Hkv > kMaxHeads || d < 1 ||
-        d > kMaxD || P < 0 || P > d / 2 || (L > 0 && B > (int64_t)0x7FFFFFFF / L))
+    if (!token_count(B, L) || Hq < 1 || Hq > kMaxHeads || Hkv < 1 || Hkv > kMaxHeads || d < 1 ||
+        d > kMaxD || P < 0 || P > d / 2)
         return FQ_ERR_SHAPE;
     if (P > 0 && table_rows != L && table_rows != B * L) return FQ_ERR_SHAPE;
     if (bits < 2 || bits > 8 || (interleaved != 0 && interleaved != 1)) return FQ_ERR_PARAM;
@@ -512,9 +519,7 @@ fq_status requant_heads_int8(const int32_t* q, int64_t B, int32_t H, int32_t L, 
                              float s_in, float s_out, int32_t zp_out, int32_t bits, int8_t* y,
                              void* stream) {
     ConsumeEvents consume;
-    if (B < 0 || L < 0 || H < 1 || H > kMaxHeads || d < 1 || d > kMaxD ||
-        (L > 0 && B > (int64_t)0x7FFFFFFF / L))
-        return FQ_ERR_SHAPE;
+    if (!token_count(B, L) || H < 1 || H > kMaxHeads || d < 1 || d > kMaxD) return FQ_ERR_SHAPE;
     if (bits < 2 || bits > 8) return FQ_ERR_PARAM;
     if (!positive(s_in) || !positive(s_out)) return FQ_ERR_PARAM;
     const int32_t half = 1 << (bits - 1);

@@ -18,21 +18,22 @@ constexpr int kBlock = 256;
 constexpr float kMagic = 12582912.0f;   // 1.5 * 2^23: v + kMagic has rint(v) in its low bits
 
 // ---------------------------------------------------------------------------
-// The table: a thread a token and pair
+// The table: a token and pair of a thread at a time
 // ---------------------------------------------------------------------------
 
 __global__ __launch_bounds__(kBlock) void rope_table_kernel(RopeTableArgs p) {
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (i >= p.T * p.P) return;
-    const int64_t tok = i / p.P;
-    const int pair = (int)(i - tok * p.P);
-    const int ax = min((int)p.axis[pair], p.axes - 1);
-    const double t = (double)p.positions[ax * p.T + tok] * p.freq[pair];
-    double s, c;
-    sincos(t, &s, &c);
-    const uint32_t lo = (uint32_t)(int)rint(16384.0 * c) & 0xFFFFu;
-    const uint32_t hi = (uint32_t)(int)rint(16384.0 * s) << 16;
-    reinterpret_cast<uint32_t*>(p.table)[i] = lo | hi;
+    const int64_t step = (int64_t)gridDim.x * kBlock;
+    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < p.T * p.P; i += step) {
+        const int64_t tok = i / p.P;
+        const int pair = (int)(i - tok * p.P);
+        const int ax = min((int)p.axis[pair], p.axes - 1);
+        const double t = (double)p.positions[ax * p.T + tok] * p.freq[pair];
+        double s, c;
+        sincos(t, &s, &c);
+        const uint32_t lo = (uint32_t)(int)rint(16384.0 * c) & 0xFFFFu;
+        const uint32_t hi = (uint32_t)(int)rint(16384.0 * s) << 16;
+        reinterpret_cast<uint32_t*>(p.table)[i] = lo | hi;
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -208,38 +209,39 @@ __global__ __launch_bounds__(kBlock) void rope_qkv_kernel(RopeArgs p, int64_t ti
     for (; h < h1; ++h) one(*reinterpret_cast<const B*>(in + h * p.d), h);
 }
 
-// Heads of any size on any base: one value a thread.
+// Heads of any size on any base: one value of a thread at a time.
 __global__ __launch_bounds__(kBlock) void rope_qkv_bytes_kernel(RopeArgs p) {
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     const int heads = p.Hq + 2 * p.Hkv;
-    const int64_t row = (int64_t)heads * p.d;
-    if (i >= p.B * p.L * row) return;
-    const int64_t tok = i / row;
-    const int at = (int)(i - tok * row);
-    const int h = at / p.d, j = at - h * p.d;
-    const int64_t b = tok / p.L;
-    const int l = (int)(tok - b * p.L);
-    if (h >= p.Hq + p.Hkv) {
-        p.v[((b * p.Hkv + h - p.Hq - p.Hkv) * p.L + l) * p.d + j] = p.qkv[i];
-        return;
-    }
-    const int x = p.qkv[i] - p.zp_x;
-    float a = (float)(x * 16384);
-    if (j < 2 * p.P) {
-        const int pair = p.interleaved ? j >> 1 : (j < p.P ? j : j - p.P);
-        const bool second = p.interleaved ? (j & 1) : j >= p.P;
-        const int off = p.interleaved ? 1 : p.P;
-        const int16_t* cs = p.table + 2 * ((p.per_image ? tok : (int64_t)l) * p.P + pair);
-        const int o = p.qkv[second ? i - off : i + off] - p.zp_x;
-        a = (float)(second ? o * cs[1] + x * cs[0] : x * cs[0] - o * cs[1]);
-    }
-    const bool is_q = h < p.Hq;
+    const int64_t row = (int64_t)heads * p.d, n = p.B * p.L * row;
     const int half = 1 << (p.bits - 1);
-    float v = __builtin_fmaf(a, is_q ? p.m_q : p.m_k, kMagic + (float)(is_q ? p.zp_q : p.zp_k));
-    v = __builtin_amdgcn_fmed3f(v, kMagic - (float)half, kMagic + (float)(half - 1));
-    int8_t* out = is_q ? p.q + ((b * p.Hq + h) * p.L + l) * p.d
-                       : p.k + ((b * p.Hkv + h - p.Hq) * p.L + l) * p.d;
-    out[j] = (int8_t)__builtin_bit_cast(uint32_t, v);
+    const int64_t step = (int64_t)gridDim.x * kBlock;
+    for (int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x; i < n; i += step) {
+        const int64_t tok = i / row;
+        const int at = (int)(i - tok * row);
+        const int h = at / p.d, j = at - h * p.d;
+        const int64_t b = tok / p.L;
+        const int l = (int)(tok - b * p.L);
+        if (h >= p.Hq + p.Hkv) {
+            p.v[((b * p.Hkv + h - p.Hq - p.Hkv) * p.L + l) * p.d + j] = p.qkv[i];
+            continue;
+        }
+        const int x = p.qkv[i] - p.zp_x;
+        float a = (float)(x * 16384);
+        if (j < 2 * p.P) {
+            const int pair = p.interleaved ? j >> 1 : (j < p.P ? j : j - p.P);
+            const bool second = p.interleaved ? (j & 1) : j >= p.P;
+            const int off = p.interleaved ? 1 : p.P;
+            const int16_t* cs = p.table + 2 * ((p.per_image ? tok : (int64_t)l) * p.P + pair);
+            const int o = p.qkv[second ? i - off : i + off] - p.zp_x;
+            a = (float)(second ? o * cs[1] + x * cs[0] : x * cs[0] - o * cs[1]);
+        }
+        const bool is_q = h < p.Hq;
+        float v = __builtin_fmaf(a, is_q ? p.m_q : p.m_k, kMagic + (float)(is_q ? p.zp_q : p.zp_k));
+        v = __builtin_amdgcn_fmed3f(v, kMagic - (float)half, kMagic + (float)(half - 1));
+        int8_t* out = is_q ? p.q + ((b * p.Hq + h) * p.L + l) * p.d
+                           : p.k + ((b * p.Hkv + h - p.Hq) * p.L + l) * p.d;
+        out[j] = (int8_t)__builtin_bit_cast(uint32_t, v);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -303,7 +305,8 @@ __global__ __launch_bounds__(kBlock) void requant_heads_kernel(RequantHeadsArgs 
     for (; h < h1; ++h) four(load(h), h);
 }
 
-unsigned blocks(int64_t n) { return (unsigned)((n + kBlock - 1) / kBlock); }
+// Workgroups of a kernel that takes one value of a thread at a time.
+unsigned blocks(int64_t n) { return (unsigned)std::min<int64_t>((n + kBlock - 1) / kBlock, 1 << 20); }
 
 // Tiles of `rows` tokens times groups of heads, a wavefront each: groups of four
 // heads where that many wavefronts are needed to fill the chip (16 a CU), longer

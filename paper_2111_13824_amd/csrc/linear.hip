@@ -19,7 +19,11 @@ __global__ __launch_bounds__(kBlock) void linear_fold_kernel(LinearFoldArgs p) {
     const int lane = threadIdx.x & 63;
     const int8_t* row = p.w + (int64_t)n * p.K;
     int sum = 0;
-    for (int k = lane; k < p.K; k += 64) sum += row[k];
+    for (int k = 16 * lane; k < p.K; k += 16 * 64) {
+        const linear::vi4 v = linear::load_tail(row, p.K, k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_sdot4(v[i], 0x01010101, sum, false);
+    }
     for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
     if (lane != 0) return;
     const double s_w = (double)p.s_w[n];

@@ -136,6 +136,35 @@ def test_heads_to_rows(fq, orc, B, H, L, d, bits, zp):  # noqa: F811
         assert intact()
 
 
+def test_offsets_beyond_32_bits(fq):  # noqa: F811
+    """The last image of a batch of more than 2^32 bytes is that image alone."""
+    import torch
+    g = torch.Generator(device="cuda:0")
+    g.manual_seed(2)
+    B, L, Hq, Hkv, d = 2500, 577, 16, 16, 64
+    table = dev(R.rope_table(np.arange(L, dtype=np.int32)[None], 0.9 ** np.arange(32),
+                             np.zeros(32, np.uint8)))
+    say("far images", B)
+    qkv = torch.randint(-128, 128, (B, L, (Hq + 2 * Hkv) * d), generator=g, device="cuda:0",
+                        dtype=torch.int8)
+    for head in (64, 37):                      # 37 of the same bytes: the kernel of single values
+        x = qkv if head == 64 else qkv.view(-1)[:B * L * 48 * 37].view(B, L, 48 * 37)
+        t = table[:, :16] if head == 37 else table
+        kw = dict(interleaved=head == 37)
+        far = fq.rope_qkv_int8(x, t.contiguous(), Hq, Hkv, 0.05, 0.07, 0.06, **kw)
+        for b in (0, B // 2, B - 1):
+            one = fq.rope_qkv_int8(x[b:b + 1].clone(), t.contiguous(), Hq, Hkv, 0.05, 0.07, 0.06, **kw)
+            for a, c in zip(far, one):
+                assert torch.equal(a[b:b + 1], c)
+        del far
+    q = qkv.view(-1)[:4 * (B // 2 * 16 * L * 64) // 4 * 4].view(torch.int32).view(-1)
+    n = q.numel() // (16 * L * 64)
+    q = q[:n * 16 * L * 64].view(n, 16, L, 64)
+    y = fq.requant_heads_int8(q, 2.0 ** -30, 0.02, 1)
+    for b in (0, n - 1):
+        assert torch.equal(y[b:b + 1], fq.requant_heads_int8(q[b:b + 1].clone(), 2.0 ** -30, 0.02, 1))
+
+
 def test_matches_the_oracle(fq, orc):  # noqa: F811
     g = np.random.default_rng(5)
     pos = g.integers(0, 5000, (3, 40)).astype(np.int32)

@@ -71,7 +71,9 @@ def test_linear_refusals(lib):
     assert call(tbits=99, zp_t=-5, zp_r=1000, mul_r=0.0) == RAN
     for k, v in (("T", -1), ("N", 0), ("K", 0), ("K", 32769), ("N", (1 << 20) + 1), ("T", 1 << 41)):
         assert call(**{k: v}) == SHAPE
-    assert call(T=1 << 24, N=1 << 20) == SHAPE      # more tiles than a grid holds
+    # fewer than 2^24 tiles of 64 x 64
+    assert call(T=(1 << 30) - 64, N=64) == RAN and call(T=(1 << 30) - 63, N=64) == SHAPE
+    assert call(T=1 << 24, N=1 << 20) == SHAPE
     for k, v in (("act", 3), ("act", -1), ("bits", 1), ("bits", 9), ("zp", 128), ("zp", -129)):
         assert call(**{k: v}) == PARAM
     assert call(bits=4, zp=8) == PARAM
@@ -110,8 +112,8 @@ def test_products_of_the_gpu_tests_reach_every_kernel(lib):
 
 def test_rope_refusals(lib):
     call = caller(lib, "rope_table_int16", pos=1, axes=3, T=5, freq=1, axis=1, P=4, table=4)
-    assert call() == RAN and call(T=0, pos=None) == EMPTY
-    for k, v in (("axes", 0), ("axes", 9), ("T", -1), ("T", 1 << 31), ("P", 0), ("P", 129)):
+    assert call() == RAN and call(T=0, pos=None) == EMPTY and call(T=1 << 25, P=128) == RAN
+    for k, v in (("axes", 0), ("axes", 9), ("T", -1), ("T", (1 << 25) + 1), ("P", 0), ("P", 129)):
         assert call(**{k: v}) == SHAPE
     assert call(table=2) == PARAM
     for k in ("pos", "freq", "axis", "table"):
@@ -121,6 +123,7 @@ def test_rope_refusals(lib):
                   rows=5, P=32, il=0, s_q=0.5, zp_q=0, s_k=0.5, zp_k=0, bits=8, q=1, k=1, v=1)
     assert call() == RAN and call(rows=10, il=1) == RAN and call(P=0, table=None, rows=0) == RAN
     assert call(B=0, qkv=None) == EMPTY and call(L=0, rows=0, q=None) == EMPTY
+    assert call(B=1 << 20, L=32, rows=32) == RAN and call(B=(1 << 20) + 1, L=32, rows=32) == SHAPE
     for k, v in (("B", -1), ("L", -1), ("Hq", 0), ("Hkv", 0), ("Hq", 1025), ("d", 0), ("d", 257),
                  ("P", -1), ("P", 33), ("rows", 4), ("rows", 6), ("rows", 20), ("B", 1 << 40)):
         assert call(**{k: v}) == SHAPE, (k, v)
