@@ -133,19 +133,26 @@ struct Shape {
     }
 };
 
-// The operands of 32 inputs and their products.
+// The operands of 32 inputs and their products.  `wa` and `xa` are the places of a
+// lane's first unit in the first blocks of its wavefront's channels and rows: those
+// of the next 32 inputs differ in bits 5 and 6 alone, and the other blocks lie
+// whole multiples of 32 rows on.
 template <class S>
 struct Part {
     vi4 a[S::FN], b[S::FT];
 
-    __device__ __forceinline__ void read(const int8_t* s, int q, int wn, int wt, int lane) {
-        const int r = lane & 31, unit = 2 * q + (lane >> 5);
+    __device__ __forceinline__ void read(const int8_t* s, int q, int wa, int xa) {
+        // worked out anew each time: kept, the places of all parts and stages are
+        // two dozen registers, which the widest tile does not have
+        asm volatile("" : "+v"(wa), "+v"(xa));
+        wa ^= 32 * q;
+        xa ^= 32 * q;
 #pragma unroll
         for (int f = 0; f < S::FN; ++f)
-            a[f] = *reinterpret_cast<const vi4*>(s + S::place(wn + 32 * f + r, unit));
+            a[f] = *reinterpret_cast<const vi4*>(s + wa + 32 * f * S::STEP);
 #pragma unroll
         for (int g = 0; g < S::FT; ++g)
-            b[g] = *reinterpret_cast<const vi4*>(s + S::BN * S::STEP + S::place(wt + 32 * g + r, unit));
+            b[g] = *reinterpret_cast<const vi4*>(s + S::BN * S::STEP + xa + 32 * g * S::STEP);
     }
     __device__ __forceinline__ void multiply(vi16 (&acc)[S::FN][S::FT]) const {
 #pragma unroll
@@ -254,6 +261,7 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
     const int n0 = (int)(tile % tiles_n) * S::BN;
     const int wn = (wave % S::WN) * 32 * FN, wt = (wave / S::WN) * 32 * FT;
     const int h = lane >> 5, K = p.K;
+    const int wa = S::place(wn + (lane & 31), h), xa = S::place(wt + (lane & 31), h);
     const int nk = (K + STEP - 1) / STEP;
 
     // The accumulators start as the folded bias.
@@ -313,12 +321,12 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 if (q + 1 < Q) {
-                    part[(q + 1) & 1].read(cur, q + 1, wn, wt, lane);
+                    part[(q + 1) & 1].read(cur, q + 1, wa, xa);
                 } else {
                     arrive<(S::NBUF - 2) * kLoads>();
                     if (ragged && k + 2 == nk) last(next);
                     fill(cur, k + S::NBUF);
-                    part[0].read(next, 0, wn, wt, lane);
+                    part[0].read(next, 0, wa, xa);
                 }
                 part[q & 1].multiply(acc);
                 interleave<S>();
@@ -332,7 +340,7 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
         if constexpr (S::NBUF == 3) fill(s2, 2);
         arrive<(S::NBUF - 1) * kLoads>();
         if (ragged && nk == 1) last(s0);
-        part[0].read(s0, 0, wn, wt, lane);
+        part[0].read(s0, 0, wa, xa);
         // the stages left over come after the loop: a way round them inside it
         // would have the compiler wait for the youngest load at its head
         int k = 0;
@@ -385,10 +393,10 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
         };
         auto all = [&](const int8_t* s) __attribute__((always_inline)) {
             Part<S> part[2];
-            part[0].read(s, 0, wn, wt, lane);
+            part[0].read(s, 0, wa, xa);
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
-                if (q + 1 < Q) part[(q + 1) & 1].read(s, q + 1, wn, wt, lane);
+                if (q + 1 < Q) part[(q + 1) & 1].read(s, q + 1, wa, xa);
                 part[q & 1].multiply(acc);
             }
         };
