@@ -21,32 +21,33 @@ enum Kernel {
 };
 
 // Products of so few rows take the kernel that shares the inputs out among the
-// wavefronts of a workgroup: K = 4096, N = 1024: 4.5 us for one row (9.0 in tiles of
-// 64 x 64), 7.3 for 32 (9.2), 8.5 for 33 (9.3), 9.8 for 48 (9.2).
+// wavefronts of a workgroup: K = 4096, N = 1024: 4.5 us for one row (10.2 in tiles of
+// 64 x 64), 6.0 for 16, 7.8 for 32 (10.2); K = 192, N = 768: 2.6 us for 32 (3.4).
 constexpr int kFewRows = 32;
 
-// What a tile costs, fitted to measurements of 130 products (T 64 .. 25088, K 192 ..
-// 4096, N 192 .. 4096): `per` workgroups share a CU; a CU's tiles take per round of
-// `per` fixed + input K microseconds, the share `few` of it at least.  Large tiles
-// move fewer bytes through L2 for a product but fill the last round worse:
-// 9232 x 1024 x 4096 takes 48 us in 464 tiles of 256 x 320 and 55 in 592 of 256 x 256;
-// 9232 x 4096 x 1024 takes 42 us in 196 tiles of 256 x 192 and 45 in 148 of 256 x 256;
-// 12608 x 768 x 2304 takes 31 us in 450 tiles of 256 x 256 and 34 in 360 of 256 x 320;
-// 788 x 768 x 768 takes 4.2 us in 156 tiles of 64 x 64 and 11.8 in 12 of 256 x 256.
-// Over the 130 the choice costs 0.2% more than the fastest tile of each.
+// What a tile costs, fitted to measurements of 136 products (T 64 .. 25088, K 192 ..
+// 32768, N 192 .. 10240, operands that were not read just before): `per` workgroups
+// share a CU; a CU's tiles take per round of `per` fixed + input K microseconds, the
+// share `few` of it at least.  Large tiles move fewer bytes through L2 for a product
+// but fill the last round worse:
+// 9232 x 1024 x 4096 takes 45 us in 464 tiles of 256 x 320 and 53 in 592 of 256 x 256;
+// 9232 x 4096 x 1024 takes 40 us in 196 tiles of 256 x 192 and 44 in 148 of 256 x 256;
+// 12608 x 768 x 2304 takes 30 us in 450 tiles of 256 x 256 and 34 in 360 of 256 x 320;
+// 788 x 768 x 768 takes 4.4 us in 156 tiles of 64 x 64 and 13 in 12 of 256 x 256.
+// Over the 136 the choice costs 0.05% more than the fastest tile of each.
 struct Cost {
     int bn, bt, per;
     float few, fixed, input;
 };
 constexpr Cost kCosts[] = {
-    {64, 64, 3, 0.52f, 2.8f, 3.9e-3f},   {128, 128, 2, 0.70f, 2.3f, 6.3e-3f},
-    {256, 128, 2, 0.60f, 3.7f, 9.2e-3f}, {256, 192, 1, 1.0f, 2.4f, 7.6e-3f},
-    {256, 256, 1, 1.0f, 3.3f, 8.5e-3f},  {256, 320, 1, 1.0f, 5.2f, 9.6e-3f},
+    {64, 64, 3, 0.33f, 2.5f, 4.6e-3f},    {128, 128, 2, 0.73f, 2.4f, 7.4e-3f},
+    {256, 128, 2, 0.64f, 3.2f, 12.4e-3f}, {256, 192, 1, 1.0f, 3.1f, 8.0e-3f},
+    {256, 256, 1, 1.0f, 3.7f, 10.2e-3f},  {256, 320, 1, 1.0f, 4.3f, 10.2e-3f},
 };
 
 // The same for the loads through registers (99 products, K 47 .. 4091, N 101 .. 4097):
-// 9232 x 1021 x 4097 takes 68 us in tiles of 256 x 256, 86 in 128 x 128 and 137 in 64 x
-// 64; 788 x 1021 x 1021 7.8 in 64 x 64, 14.9 in 128 x 128 and 24.9 in 256 x 256.
+// 9232 x 1021 x 4097 takes 81 us in tiles of 256 x 256, 100 in 128 x 128 and 143 in 64
+// x 64; 788 x 1021 x 1021 9.3 in 64 x 64, 15 in 128 x 128 and 25 in 256 x 256.
 constexpr Cost kCostsR[] = {
     {64, 64, 3, 0.51f, 2.1f, 14.1e-3f},
     {128, 128, 2, 0.92f, 7.6f, 9.1e-3f},

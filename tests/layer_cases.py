@@ -89,11 +89,13 @@ KERNELS = ("rows16", "rows32", "tile64", "tile128", "tile256x128", "tile256x192"
 PRODUCTS = {
     "rows16": [(5, 80, 300), (16, 1001, 77)],
     "rows32": [(17, 80, 300), (32, 1001, 77), (31, 64, 16)],
-    "tile64": [(100, 80, 300), (33, 16, 70), (1000, 400, 1001), (500, 384, 64)],
-    "tile128": [(1130, 80, 1001), (1260, 48, 1001), (2170, 272, 1001), (1000, 400, 2050)],
-    "tile256x128": [(4120, 80, 1001), (1000, 48, 4100), (4120, 272, 1001), (2170, 128, 3000)],
+    "tile64": [(100, 80, 300), (33, 16, 70), (1000, 400, 1001), (500, 384, 64),
+               (1130, 80, 1001), (1260, 48, 1001)],
+    "tile128": [(1000, 80, 2050), (1000, 48, 2050), (2170, 272, 1001), (1000, 400, 2050)],
+    "tile256x128": [(4120, 80, 1001), (1000, 48, 4100), (4120, 272, 1001), (2170, 128, 3000),
+                    (5420, 80, 2050), (5550, 48, 2050), (5420, 208, 2050)],
     "tile256x192": [(3860, 80, 2050), (2690, 48, 3000), (3860, 272, 2050), (3860, 192, 2050)],
-    "tile256x256": [(5420, 80, 2050), (5550, 48, 2050), (5420, 208, 2050), (5420, 256, 2050)],
+    "tile256x256": [(5420, 256, 2050), (5420, 272, 2050), (5550, 400, 2050), (5420, 336, 2050)],
     "tile256x320": [(7760, 80, 2050), (7370, 208, 2050), (7370, 400, 2050), (7760, 320, 2050)],
     "tile64r": [(100, 49, 70), (230, 301, 70), (33, 7, 5), (70, 129, 66)],
     "tile128r": [(2960, 131, 2050), (2050, 301, 2050), (4130, 301, 1001)],
