@@ -7,7 +7,7 @@ namespace fqvit {
 namespace linear {
 
 enum Kernel {
-    kRows16,        // linear_rows.hip: up to 16 rows of x, up to 32
+    kRows16,        // linear_rows.hip: 16 rows of x a workgroup, 32
     kRows32,
     kTile64,        // linear_tile.h: channels x rows 64 x 64, 128 x 128,
     kTile128,
@@ -20,10 +20,21 @@ enum Kernel {
     kTile256R,
 };
 
-// Products of so few rows take the kernel that shares the inputs out among the
-// wavefronts of a workgroup: K = 4096, N = 1024: 4.5 us for one row (10.2 in tiles of
-// 64 x 64), 6.0 for 16, 7.8 for 32 (10.2); K = 192, N = 768: 2.6 us for 32 (3.4).
-constexpr int kFewRows = 32;
+// Few rows: the kernels that share the inputs out among the wavefronts of a workgroup
+// (16 channels x 16 or 32 rows) finish a product sooner than tiles of 64 x 64, which take
+// K one step after another, until their workgroups come to several a CU.  Microseconds,
+// fitted to 160 products (T 33 .. 1576, K 192 .. 8192, N 64 .. 4096): 0.2% over the
+// fastest of the three, where tiles alone took 26% more.  K = 4096, N = 1024: 5.9 in 16
+// rows, 7.7 in 32 and 10.2 in tiles for T = 48, 9.5, 7.8 and 10.7 for 96, 15.5, 13.2 and
+// 10.9 for 197; K = 768, N = 192: 3.1, 3.4 and 4.2 for 197, 4.4, 4.4 and 4.3 for 788.
+// Without whole units: K = 1001, N = 300: 4.5, 5.6 and 7.9 for 197, 9.8, 8.4 and 8.0 for 788.
+struct FewCost {
+    float fixed, round, input;      // round + input K: 256 workgroups more
+};
+constexpr FewCost kFew[2][3] = {    // 16 rows, 32 rows, a round of tiles of 64 x 64
+    {{2.3f, 0.08f, 1.9e-3f}, {2.25f, 0.14f, 2.8e-3f}, {2.9f, 0.0f, 4.8e-3f}},
+    {{2.3f, 0.08f, 0.85e-3f}, {2.25f, 0.14f, 1.22e-3f}, {2.9f, 0.0f, 1.8e-3f}},     // whole units
+};
 
 // What a tile costs, fitted to measurements of 136 products (T 64 .. 25088, K 192 ..
 // 32768, N 192 .. 10240, operands that were not read just before): `per` workgroups
@@ -71,13 +82,24 @@ int cheapest(const LinearArgs& a, const Cost (&costs)[shapes]) {
     return best;
 }
 
+inline int64_t ceil_div(int64_t a, int b) { return (a + b - 1) / b; }
+
 // Rows of whole 16-byte units on 16-byte aligned bases can be loaded straight into
 // LDS.
 inline Kernel plan(const LinearArgs& a) {
     if (a.T <= 16) return kRows16;
-    if (a.T <= kFewRows) return kRows32;
     const bool units = a.K % 16 == 0 &&
                        ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15) == 0;
+    if (a.T <= 32 || ceil_div(a.T, 64) * ceil_div(a.N, 64) <= 256) {
+        float cost[3];
+        for (int i = 0; i < 3; ++i) {
+            const FewCost& c = kFew[units][i];
+            const int64_t blocks = i < 2 ? ceil_div(a.N, 16) * ceil_div(a.T, 16 << i) : 1;
+            cost[i] = c.fixed + (float)ceil_div(blocks, 256) * (c.round + c.input * (float)a.K);
+        }
+        if (a.T <= 32 || cost[0] < cost[2] || cost[1] < cost[2])
+            return cost[0] < cost[1] ? kRows16 : kRows32;
+    }
     return units ? (Kernel)(kTile64 + cheapest(a, kCosts))
                  : (Kernel)(kTile64R + cheapest(a, kCostsR));
 }

@@ -1,5 +1,5 @@
-// Linear layers of a few rows of x (one token, a small batch) for gfx950: what
-// counts is reading the weights once, with every CU's loads under way at once.
+// Linear layers of a few rows of x (one token, a small image) for gfx950: what
+// counts is that every CU's loads are under way at once.
 //
 // A workgroup of eight wavefronts takes 16 channels; the wavefronts share the
 // inputs, 64 of each row at a time, and load the weights from global memory

@@ -181,12 +181,15 @@ __device__ __forceinline__ void arrive() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// A matrix's rows from `row0` on as a buffer: reads beyond its end give nothing.
+// A matrix's rows from `row0` on as a buffer of at most kNone bytes (a tile's are
+// 10 MiB at most): reads beyond its end give nothing.
+constexpr unsigned kNone = 0x70000000u;
+
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const int8_t* m, int64_t rows, int64_t row0,
                                                           int K) {
     const int64_t bytes = (rows - row0) * K;
     return __builtin_amdgcn_make_buffer_rsrc((void*)(m + row0 * K), (short)0,
-                                             (int)(bytes < 0x7FFFFFFF ? bytes : 0x7FFFFFFF), 0x00020000);
+                                             (int)(bytes < kNone ? bytes : kNone), 0x00020000);
 }
 
 // One load of 16 bytes a lane from a buffer straight into LDS: the wavefront's
@@ -285,14 +288,13 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
 
     if constexpr (S::DMA) {
         const __amdgpu_buffer_rsrc_t wr = rows_of(p.w, p.N, n0, K), xr = rows_of(p.x, p.T, t0, K);
-        // an offset outside every buffer: nothing is read, and the loads that
-        // arrive() counts stay the same
-        constexpr unsigned kNone = 0x70000000u;
         constexpr int U = S::UN > S::UT ? S::UN : S::UT;
         unsigned off[U];
 #pragma unroll
         for (int i = 0; i < U; ++i) off[i] = S::fill_row(t, i) * K + S::fill_unit(t, i) * 16;
         auto fill = [&](int8_t* s, int k) __attribute__((always_inline)) {
+            // past the last stage: outside the buffers, nothing is read, and the loads
+            // that arrive() counts stay the same
             const unsigned k0 = k < nk ? k * STEP : kNone;
 #pragma unroll
             for (int i = 0; i < S::UN; ++i)
@@ -568,7 +570,7 @@ typedef Shape<4, 2, 2, 4, 64, 2, false, 1> Tile256R;
 template <class S>
 void launch_tiles(const LinearArgs& a, hipStream_t stream);
 
-// Up to 16 FT rows of x (linear_rows.hip).
+// 16 FT rows of x a workgroup (linear_rows.hip).
 template <int FT>
 void launch_rows(const LinearArgs& a, hipStream_t stream);
 

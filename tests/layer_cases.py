@@ -87,17 +87,19 @@ def layer(T, K, N, seed, zp_x=0, spread=36.0):
 KERNELS = ("rows16", "rows32", "tile64", "tile128", "tile256x128", "tile256x192", "tile256x256",
            "tile256x320", "tile64r", "tile128r", "tile256r")
 PRODUCTS = {
-    "rows16": [(5, 80, 300), (16, 1001, 77)],
-    "rows32": [(17, 80, 300), (32, 1001, 77), (31, 64, 16)],
-    "tile64": [(100, 80, 300), (33, 16, 70), (1000, 400, 1001), (500, 384, 64),
-               (1130, 80, 1001), (1260, 48, 1001)],
+    "rows16": [(5, 80, 300), (16, 1001, 77), (17, 80, 300), (32, 1001, 77), (31, 64, 16), (100, 80, 300),
+               (33, 16, 70), (500, 384, 64), (100, 49, 70), (230, 301, 70), (33, 7, 5), (70, 129, 66)],
+    "rows32": [(97, 48, 1900), (24, 64, 4100), (32, 1001, 4097), (20, 7, 4099), (128, 1024, 1001),
+               (394, 4096, 200), (250, 1001, 300)],
+    "tile64": [(640, 80, 1000), (1000, 400, 1001), (1030, 16, 1000), (1130, 80, 1001), (1260, 48, 1001),
+               (900, 384, 700), (300, 1024, 520), (1300, 16, 1290)],
     "tile128": [(1000, 80, 2050), (1000, 48, 2050), (2170, 272, 1001), (1000, 400, 2050)],
     "tile256x128": [(4120, 80, 1001), (1000, 48, 4100), (4120, 272, 1001), (2170, 128, 3000),
                     (5420, 80, 2050), (5550, 48, 2050), (5420, 208, 2050)],
     "tile256x192": [(3860, 80, 2050), (2690, 48, 3000), (3860, 272, 2050), (3860, 192, 2050)],
     "tile256x256": [(5420, 256, 2050), (5420, 272, 2050), (5550, 400, 2050), (5420, 336, 2050)],
     "tile256x320": [(7760, 80, 2050), (7370, 208, 2050), (7370, 400, 2050), (7760, 320, 2050)],
-    "tile64r": [(100, 49, 70), (230, 301, 70), (33, 7, 5), (70, 129, 66)],
+    "tile64r": [(1000, 49, 700), (1500, 301, 500), (1300, 129, 666), (1400, 7, 1290), (900, 65, 1001)],
     "tile128r": [(2960, 131, 2050), (2050, 301, 2050), (4130, 301, 1001)],
     "tile256r": [(4000, 49, 2050), (3870, 131, 2050), (4130, 65, 2050)],
 }

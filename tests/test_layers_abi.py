@@ -106,7 +106,7 @@ def test_products_of_the_gpu_tests_reach_every_kernel(lib):
             assert R.KERNELS[lib.fq_test_linear_kernel()] == name, (name, T, K, N)
     # rows of whole units on other bases take the register path
     for x, w in ((20, 16), (16, 24)):
-        call(T=100, K=64, N=64, x=x, w=w)
+        call(T=1000, K=64, N=1000, x=x, w=w)
         assert R.KERNELS[lib.fq_test_linear_kernel()] == "tile64r"
 
 

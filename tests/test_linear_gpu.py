@@ -104,6 +104,18 @@ def test_channels(fq, N, T, K):
     run(fq, R.layer(T, K, N, seed=N))
 
 
+@pytest.mark.parametrize("T,K,N", [(T, 64, 1000) for T in (1025, 1026, 1055, 1057, 1087, 1088)]
+                         + [(T, 67, 1000) for T in (1023, 1024, 1025, 1056, 1087)]
+                         + [(1000, K, 1000) for K in (1, 2, 15, 16, 17, 31, 32, 33, 48, 63, 65, 96, 112, 127,
+                                                      128, 129, 144, 240, 255, 256, 257, 272, 400, 528)]
+                         + [(1000, K, N) for K in (64, 70)
+                            for N in (1001, 1002, 1003, 1007, 1009, 1023, 1025, 1039, 1057, 1087, 1088)])
+def test_edges_of_small_tiles(fq, T, K, N):
+    """Rows, inputs and channels that end inside tiles of 64 x 64."""
+    say("small tiles", T, K, N)
+    run(fq, R.layer(T, K, N, seed=T + K + N, zp_x=6), residual=True, zp_y=-4, seed=K)
+
+
 @pytest.mark.parametrize("act", ["none", "relu", "table"])
 @pytest.mark.parametrize("residual", [False, True])
 @pytest.mark.parametrize("T,K,N", [(1, 128, 256), (40, 96, 100), (130, 192, 260), (600, 64, 512),
@@ -139,14 +151,16 @@ def test_every_kernel_and_epilogue(fq, name, act, residual):
 
 
 @pytest.mark.parametrize("offset", [1, 2, 4, 8, 12, 15])
-@pytest.mark.parametrize("T,K,N", [(1, 64, 64), (9, 48, 20), (150, 128, 132), (260, 100, 64)])
+@pytest.mark.parametrize("T,K,N", [(1, 64, 64), (9, 48, 20), (150, 128, 132), (260, 100, 64),
+                                   (1000, 128, 1001), (1100, 100, 700)])
 def test_unaligned_bases(fq, offset, T, K, N):
     say("offset", offset, T, K, N)
     run(fq, R.layer(T, K, N, seed=offset), "relu", True, 1, 8, offset, seed=T)
 
 
 @pytest.mark.parametrize("T,K,N", [(1, 64, 64), (13, 100, 37), (70, 701, 1001), (300, 256, 256),
-                                   (129, 16, 4), (1, 32768, 3), (65, 32768, 65), (2100, 128, 1024)])
+                                   (129, 16, 4), (1, 32768, 3), (65, 32768, 65), (2100, 128, 1024),
+                                   (1000, 272, 1001), (1100, 101, 700)])
 def test_accumulators(fq, T, K, N):
     say("int32", T, K, N)
     p = R.layer(T, K, N, seed=K)
@@ -180,6 +194,19 @@ def test_extremes(fq, T):
                 got = host(fq.linear_int8(dev(x), dev(w), dev(f), dev(mul), 3, **kd))
                 with np.errstate(over="ignore"):
                     assert np.array_equal(got, R.linear(x, w, f, mul, 3, **kw)), (m, list(kw))
+
+
+@pytest.mark.parametrize("T,N", [(1, 70), (4200, 130), (2600, 2050), (5500, 2050)])
+def test_largest_sums(fq, T, N):
+    """Every row the same, so one row of the plain form is the reference."""
+    import torch
+    K = 32768
+    say("largest sums", T, N)
+    x = torch.full((T, K), -128, dtype=torch.int8, device="cuda:0")
+    w = np.where(np.arange(N)[:, None] % 2, -128, 127).astype(np.int8) * np.ones((1, K), np.int8)
+    f = np.where(np.arange(N) % 2, 2 ** 30, -2 ** 30).astype(np.int32)
+    got = host(fq.linear_int32(x, dev(w), dev(f)))
+    assert (got == R.sums(np.full((1, K), -128, np.int8), w, f)).all()
 
 
 @pytest.mark.parametrize("T", [3, 40, 300])
@@ -233,7 +260,8 @@ def test_fold(fq, orc, K):
         assert np.array_equal(host(f), rf) and np.array_equal(host(m), rm)
 
 
-@pytest.mark.parametrize("T,K,N", [(5, 64, 48), (200, 64, 192), (600, 128, 512), (90, 50, 27)])
+@pytest.mark.parametrize("T,K,N", [(5, 64, 48), (200, 64, 192), (600, 128, 512), (90, 50, 27), (1100, 64, 700),
+                                   (1000, 50, 1001)])
 def test_output_over_the_residual(fq, T, K, N):
     say("in place", T, K, N)
     p = R.layer(T, K, N, seed=1)
