@@ -8,6 +8,7 @@
 #include <cstdint>
 
 #include "fqvit_internal.h"
+#include "layers_internal.h"
 
 namespace {
 

@@ -9,6 +9,7 @@
 #include "bytes_device.h"
 #include "fqvit.h"
 #include "fqvit_launch.h"
+#include "layers_internal.h"
 #include "requant_device.h"
 
 namespace fqvit {

@@ -1,7 +1,7 @@
 // Which kernel a linear layer's product takes (host code only).
 #pragma once
 
-#include "fqvit_internal.h"
+#include "layers_internal.h"
 
 namespace fqvit {
 namespace linear {

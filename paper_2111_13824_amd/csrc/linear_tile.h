@@ -5,6 +5,7 @@
 #include "bytes_device.h"
 #include "fqvit.h"
 #include "fqvit_launch.h"
+#include "layers_internal.h"
 
 namespace fqvit {
 namespace linear {

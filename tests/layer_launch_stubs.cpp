@@ -1,7 +1,7 @@
 // Test-only stand-ins for the launchers of the linear layers, the rotary
 // positions and the heads' way back to rows: each keeps what the C ABI's host
 // code passed it and launches nothing (tests/test_layers_abi.py).
-#include "fqvit_internal.h"
+#include "layers_internal.h"
 #include "linear_plan.h"
 
 namespace fqvit {
