@@ -2,8 +2,8 @@
 // heads back to rows, for gfx950.  Both move each byte once and are bound by
 // memory: what counts is that rows are read and written in whole lines with many
 // loads under way.  On ViT-L/16 at batch 16 (9232 rows of 48 heads of 64, 57 MB) the
-// rotation takes 11.9 us, 4.8 TB/s; on ViT-B/16 at batch 64 the way back to rows
-// (48 MB) 8.6 to 9.1 us, 5.5 TB/s; a large copy reaches 5.1.
+// rotation takes 12.0 us, 4.7 TB/s; on ViT-B/16 at batch 64 the way back to rows
+// (48 MB) 9.2 us, 5.2 TB/s; a large copy reaches 5.1.
 #include <algorithm>
 
 #include "bytes_device.h"
