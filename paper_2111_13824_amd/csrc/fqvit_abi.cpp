@@ -457,9 +457,11 @@ fq_status fq_activation_table(int32_t kind, float s_t, int32_t zp_t, int32_t tab
             f = t < -700.0 ? 0.0 : t / (1.0 + std::exp(-t));   // exp's range ends at 709
         return f / (double)s_y;
     };
-    // the magnitude grows towards the two ends
+    // GELU and SiLU have an extremum inside: every value is checked, and none is
+    // written unless all can be
     const int last = (1 << table_bits) - 1;
-    if (!(std::fabs(value(0)) <= 3.4e38) || !(std::fabs(value(last)) <= 3.4e38)) return FQ_ERR_PARAM;
+    for (int u = 0; u <= last; ++u)
+        if (!(std::fabs(value(u)) <= 3.4028234663852886e38)) return FQ_ERR_PARAM;
     for (int u = 0; u <= last; ++u) table[u] = (float)value(u);
     return FQ_OK;
 }

@@ -210,6 +210,24 @@ def test_activation_tables(lib):
     assert lib.fq_activation_table(0, 1.0, 0, 4, 1.0, None) == B.FQ_ERR_NULL
 
 
+@pytest.mark.parametrize("kind", [0, 1, 2])
+def test_activation_tables_beyond_binary32(lib, kind):
+    """A table whose ends are small and whose middle, near the function's
+    extremum below 0, is beyond binary32 in steps of the output; one whose end
+    is; and the largest that fit.  A refused table is left as it was."""
+    table = np.full(4096, 7, np.float32)
+    for s_t, zp, s_y in ((0.01, 4095, 1e-42), (0.01, 0, 1e-42), (0.01, 4095, 2.0 ** -131)):
+        assert lib.fq_activation_table(kind, s_t, zp, 12, s_y, table.ctypes.data) == B.FQ_ERR_PARAM
+        assert (table == 7).all()
+    # the extrema are -0.17 and -0.28: in steps of 2^-129 below 2^128
+    assert lib.fq_activation_table(kind, 0.01, 4095, 12, 2.0 ** -129, table.ctypes.data) == B.FQ_OK
+    assert np.isfinite(table).all() and table.min() < -2.0 ** 126
+    # exactly the largest finite value: f(t) = t far above 0
+    big = float(np.finfo(np.float32).max)
+    assert lib.fq_activation_table(kind, big / 4, 11, 4, 1.0, table.ctypes.data) == B.FQ_OK
+    assert np.isfinite(table).all() and table[15] == np.float32(big)
+
+
 @pytest.mark.skipif(bool(SAN_LIB), reason="needs torch, which the sanitizer run leaves out")
 def test_binding_refusals(lib, monkeypatch):
     """Dtypes, shapes and layouts, then the device."""
