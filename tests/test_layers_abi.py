@@ -110,6 +110,28 @@ def test_products_of_the_gpu_tests_reach_every_kernel(lib):
         assert R.KERNELS[lib.fq_test_linear_kernel()] == "tile64r"
 
 
+# channels, rows and threads of a workgroup
+WORKGROUPS = dict(rows16=(16, 16, 512), rows32=(16, 32, 512), tile64=(64, 64, 256), tile128=(128, 128, 256),
+                  tile256x128=(256, 128, 512), tile256x192=(256, 192, 512), tile256x256=(256, 256, 512),
+                  tile256x320=(256, 320, 512), tile64r=(64, 64, 256), tile128r=(128, 128, 256),
+                  tile256r=(256, 256, 512))
+
+
+@pytest.mark.parametrize("x", [16, 17])
+def test_no_launch_has_more_threads_than_the_hardware_takes(lib, x):
+    """The sizes that the entry points allow, up to their limits: fewer than 2^32
+    threads a launch, in whichever kernel the product takes."""
+    import layer_cases as R
+    call = caller(lib, "linear_int32", x=x, T=1, w=16, N=1, K=16, fold=None, out=1)
+    for N in (1, 64, 65, 128, 192, 256, 257, 1000, 4096, 1 << 16, 1 << 20):
+        most = ((1 << 24) - 1) // (-(-N // 64)) * 64
+        for T in (most, most - 63, most - 64, most // 2, most // 2 + 1, most // 64, 17, 16):
+            for K in (16, 128, 4096, 32768):
+                assert call(T=T, N=N, K=K) == RAN
+                bn, bt, threads = WORKGROUPS[R.KERNELS[lib.fq_test_linear_kernel()]]
+                assert -(-N // bn) * -(-T // bt) * threads < 1 << 32, (T, K, N)
+
+
 def test_rope_refusals(lib):
     call = caller(lib, "rope_table_int16", pos=1, axes=3, T=5, freq=1, axis=1, P=4, table=4)
     assert call() == RAN and call(T=0, pos=None) == EMPTY and call(T=1 << 25, P=128) == RAN
