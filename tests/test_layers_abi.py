@@ -313,6 +313,44 @@ def test_binding_refusals(lib, monkeypatch):
         fq.requant_heads_int8(z(2, 3, 5, 8, dtype=i32), 1.0, 1.0, 0, y=z(2, 5, 25))
 
 
+def test_the_binding_cuts_no_integer(lib, monkeypatch):
+    """ctypes keeps the low 32 bits of an integer: a row of 2^32 + 16 inputs would
+    be a row of 16.  Sizes and scalars beyond 32 bits are refused, in every entry
+    point, and reach no launcher; the ends of the range go through."""
+    monkeypatch.setattr(B, "_lib", lib)
+    good = (16, 1, 16, 3, 16, None, 16, 0)             # x, T, w, N, K, fold, out, stream
+    n = lib.fq_test_layer_calls()
+    for prepare in (False, True):
+        for at in (3, 4):
+            for bad in (2 ** 32 + 16, -2 ** 32 + 16, 2 ** 31, -2 ** 31 - 1, 2 ** 70):
+                args = (*good[:at], bad, *good[at + 1:])
+                with pytest.raises(ValueError, match="32-bit"):
+                    B._invoke("linear_int32", args, (), prepare, None)
+        for end in (2 ** 31 - 1, -2 ** 31):
+            with pytest.raises(B.FqError):
+                call = B._invoke("linear_int32", (*good[:3], end, *good[4:]), (), prepare, None)
+                call()
+    assert lib.fq_test_layer_calls() == n
+    B._invoke("linear_int32", good, (), False, None)
+    assert lib.fq_test_layer_calls() == n + 1
+    for name, types in B.SIGNATURES.items():
+        narrow = [i for i, t in enumerate(types) if t is ctypes.c_int32]
+        assert len(narrow) > 1
+        for at in narrow:
+            args = [2 ** 32 + 1 if i == at else 1 for i in range(len(types))]
+            with pytest.raises(ValueError, match="32-bit"):
+                B._narrow(name, args)
+    # what is no integer is left to ctypes
+    with pytest.raises(ctypes.ArgumentError):
+        B._invoke("linear_int32", (*good[:3], 3.0, *good[4:]), (), False, None)
+    if SAN_LIB:                                        # that run leaves torch out
+        return
+    pytest.importorskip("torch")
+    import paper_2111_13824_amd as fq
+    with pytest.raises(ValueError, match="32-bit"):
+        fq.activation_table("gelu", 1.0, 1.0, zp_t=2 ** 32 + 8, table_bits=4, device="cpu")
+
+
 @pytest.mark.skipif(bool(SAN_LIB), reason="this is the run that starts it")
 def test_host_code_under_sanitizers(tmp_path):
     from test_sanitizers import SAN, _env
