@@ -248,6 +248,18 @@ def _raw_stream(stream, device: int) -> int:
     return torch._C._cuda_getCurrentRawStream(device)
 
 
+def _empty(stream, shape, dtype, device):
+    """An output or workspace that the caller did not give, from the memory of the
+    stream that the call runs on: torch's allocator then hands it on only behind
+    that stream's work (memory of the current stream could still be in use there
+    when another stream writes it, or be handed on while that stream still does)."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def ptf_layernorm_int8(x_q, zp_in: int, alpha, K: int, gamma, beta, s_out: float, zp_out: int,
                        bits: int = 8, y_q=None, stream=None, prepare: bool = False):
     """PTF LayerNorm of an int8 [T, C] tensor; returns (or fills) int8 [T, C].
@@ -255,7 +267,7 @@ def ptf_layernorm_int8(x_q, zp_in: int, alpha, K: int, gamma, beta, s_out: float
     import torch
     T, C = x_q.shape
     if y_q is None:
-        y_q = torch.empty_like(x_q)
+        y_q = _empty(stream, x_q.shape, x_q.dtype, x_q.device)
     if alpha.shape != (C,) or gamma.shape != (C,) or beta.shape != (C,) or y_q.shape != (T, C):
         raise ValueError("alpha, gamma, beta must be [C] and y_q [T, C]")
     args = (_dev_ptr(x_q, torch.int8, "x_q", 2), T, C, zp_in,
@@ -280,7 +292,7 @@ def lis_softmax_log4(logits, s_logit: float, bits: int = 4, exp_n: int = 20, bia
     if codes is None:
         # rows without padding: the kernel writes every byte (an odd row's last
         # high nibble 0)
-        codes = torch.empty((G, Lq, codes_ld(Lk, bits)), dtype=torch.uint8, device=logits.device)
+        codes = _empty(stream, (G, Lq, codes_ld(Lk, bits)), torch.uint8, logits.device)
     if codes.dim() != 3 or codes.shape[:2] != (G, Lq):
         raise ValueError("codes must be [G, Lq, ld_codes]")
     Hb = 0
@@ -303,7 +315,7 @@ def lis_attn_v_shift(codes, v, Lk: int, zp_v: int = 0, bits: int = 4, out=None, 
     if v.dim() != 3 or v.shape[:2] != (G, Lk):
         raise ValueError("v must be [G, Lk, d]")
     if out is None:
-        out = torch.empty((G, Lq, d), dtype=torch.int32, device=v.device)
+        out = _empty(stream, (G, Lq, d), torch.int32, v.device)
     if out.shape != (G, Lq, d):
         raise ValueError("out must be [G, Lq, d]")
     args = (_dev_ptr(codes, torch.uint8, "codes", 3), ld, _dev_ptr(v, torch.int8, "v", 3), zp_v,
@@ -321,7 +333,7 @@ def lis_attn_v_shift_wide(codes, v, Lk: int, zp_v: int = 0, bits: int = 8, out=N
     if v.dim() != 3 or v.shape[:2] != (G, Lk):
         raise ValueError("v must be [G, Lk, d]")
     if out is None:
-        out = torch.empty((G, Lq, d), dtype=torch.int64, device=v.device)
+        out = _empty(stream, (G, Lq, d), torch.int64, v.device)
     if out.shape != (G, Lq, d):
         raise ValueError("out must be [G, Lq, d]")
     args = (_dev_ptr(codes, torch.uint8, "codes", 3), ld, _dev_ptr(v, torch.int8, "v", 3), zp_v,
@@ -338,7 +350,7 @@ def lis_attention_head(logits, v, s_logit: float, bits: int = 4, exp_n: int = 20
     if v.dim() != 3 or v.shape[:2] != (G, Lk):
         raise ValueError("v must be [G, Lk, d]")
     if out is None:
-        out = torch.empty((G, Lq, d), dtype=torch.int32, device=logits.device)
+        out = _empty(stream, (G, Lq, d), torch.int32, logits.device)
     if out.shape != (G, Lq, d):
         raise ValueError("out must be [G, Lq, d]")
     Hb = 0
@@ -371,12 +383,12 @@ def ptf_calibrate(x, bits: int = 8, K: int = 3, s=None, zp=None, alpha=None, wor
     import torch
     T, C = x.shape
     dev = x.device
-    s = torch.empty(1, dtype=torch.float64, device=dev) if s is None else s
-    zp = torch.empty(1, dtype=torch.int32, device=dev) if zp is None else zp
-    alpha = torch.empty(C, dtype=torch.uint8, device=dev) if alpha is None else alpha
+    s = _empty(stream, 1, torch.float64, dev) if s is None else s
+    zp = _empty(stream, 1, torch.int32, dev) if zp is None else zp
+    alpha = _empty(stream, C, torch.uint8, dev) if alpha is None else alpha
     need = ptf_calibrate_workspace_bytes(T, C, K) if T > 0 else 0
     if workspace is None:
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+        workspace = _empty(stream, max(need, 1), torch.uint8, dev)
     args = (_dev_ptr(x, torch.float32, "x", 2), T, C, bits, K,
             _dev_ptr(s, torch.float64, "s", 1), _dev_ptr(zp, torch.int32, "zp", 1),
             _dev_ptr(alpha, torch.uint8, "alpha", 1), _dev_ptr(workspace, torch.uint8, "workspace", 1),
@@ -392,9 +404,9 @@ def ptf_calibrate_noalloc(x, bits: int = 8, K: int = 3, s=None, zp=None, alpha=N
     import torch
     T, C = x.shape
     dev = x.device
-    s = torch.empty(1, dtype=torch.float64, device=dev) if s is None else s
-    zp = torch.empty(1, dtype=torch.int32, device=dev) if zp is None else zp
-    alpha = torch.empty(C, dtype=torch.uint8, device=dev) if alpha is None else alpha
+    s = _empty(stream, 1, torch.float64, dev) if s is None else s
+    zp = _empty(stream, 1, torch.int32, dev) if zp is None else zp
+    alpha = _empty(stream, C, torch.uint8, dev) if alpha is None else alpha
     args = (_dev_ptr(x, torch.float32, "x", 2), T, C, bits, K,
             _dev_ptr(s, torch.float64, "s", 1), _dev_ptr(zp, torch.int32, "zp", 1),
             _dev_ptr(alpha, torch.uint8, "alpha", 1), _stream(stream, x))
@@ -408,7 +420,7 @@ def ptf_quantize_int8(x, s, zp, alpha, bits: int = 8, x_q=None, stream=None,
     import torch
     T, C = x.shape
     if x_q is None:
-        x_q = torch.empty((T, C), dtype=torch.int8, device=x.device)
+        x_q = _empty(stream, (T, C), torch.int8, x.device)
     if alpha.shape != (C,) or x_q.shape != (T, C):
         raise ValueError("alpha must be [C] and x_q [T, C]")
     args = (_dev_ptr(x, torch.float32, "x", 2), T, C, _dev_ptr(s, torch.float64, "s", 1),
@@ -423,7 +435,7 @@ def requant_dyadic_int8(q, s_in: float, s_out: float, zp_out: int, bits: int = 8
     int8 container; returns (or fills) int8 of the same shape."""
     import torch
     if y is None:
-        y = torch.empty(q.shape, dtype=torch.int8, device=q.device)
+        y = _empty(stream, q.shape, torch.int8, q.device)
     if y.shape != q.shape:
         raise ValueError("y must have the shape of q")
     args = (_dev_ptr(q, torch.int32, "q"), q.numel(), s_in, s_out, zp_out, bits,
@@ -443,7 +455,7 @@ def lis_attention_qk(q, k, v, s_logit: float, zp_q: int = 0, zp_k: int = 0, bits
     if k.shape != (G, Lk, dk) or v.shape[:2] != (G, Lk):
         raise ValueError("k must be [G, Lk, dk] and v [G, Lk, d]")
     if out is None:
-        out = torch.empty((G, Lq, d), dtype=torch.int32, device=q.device)
+        out = _empty(stream, (G, Lq, d), torch.int32, q.device)
     Hb = bias.shape[0] if bias is not None else 0
     args = (_dev_ptr(q, torch.int8, "q", 3), _dev_ptr(k, torch.int8, "k", 3), zp_q, zp_k, dk,
             _dev_ptr(bias, torch.int32, "bias", 3), Hb, G, Lq, Lk, s_logit, bits, exp_n,
@@ -463,9 +475,9 @@ def linear_fold_int8(w, s_w, s_x: float, s_y: float = 1.0, zp_x: int = 0, bias=N
     N, K = _dims(w, 2, "w")
     dev = w.get_device()
     if fold is None:
-        fold = torch.empty(N, dtype=torch.int32, device=w.device)
+        fold = _empty(stream, N, torch.int32, w.device)
     if mul is None:
-        mul = torch.empty(N, dtype=torch.float32, device=w.device)
+        mul = _empty(stream, N, torch.float32, w.device)
     specs = [("w", w, torch.int8, (N, K)), ("s_w", s_w, torch.float32, (N,)),
              ("fold", fold, torch.int32, (N,)), ("mul", mul, torch.float32, (N,))]
     if bias is not None:
@@ -505,7 +517,7 @@ def linear_int8(x, w, fold, mul, zp_y: int = 0, bits: int = 8, relu: bool = Fals
     elif relu:
         act = ACT_RELU
     if y is None:
-        y = x.new_empty((T, N))
+        y = x.new_empty((T, N)) if stream is None else _empty(stream, (T, N), i8, x.device)
     try:
         fits = (x.dtype is i8 and x.is_contiguous() and dev >= 0
                 and w.dtype is i8 and w.shape == (N, K) and w.is_contiguous()
@@ -542,7 +554,7 @@ def linear_int32(x, w, fold=None, out=None, stream=None, prepare: bool = False):
     N = w.shape[0]
     dev = x.get_device()
     if out is None:
-        out = torch.empty((T, N), dtype=i32, device=x.device)
+        out = _empty(stream, (T, N), i32, x.device)
     try:
         fits = (x.dtype is i8 and x.is_contiguous() and dev >= 0
                 and w.dtype is i8 and w.shape == (N, K) and w.is_contiguous()
@@ -588,7 +600,7 @@ def rope_table_int16(positions, freq, axis, table=None, stream=None, prepare: bo
     P, = _dims(freq, 1, "freq")
     dev = positions.get_device()
     if table is None:
-        table = torch.empty((T, P, 2), dtype=i16, device=positions.device)
+        table = _empty(stream, (T, P, 2), i16, positions.device)
     try:
         fits = (positions.dtype is i32 and positions.is_contiguous() and dev >= 0
                 and freq.dtype is f64 and freq.is_contiguous() and freq.get_device() == dev
@@ -622,12 +634,13 @@ def rope_qkv_int8(qkv, table, Hq: int, Hkv: int, s_x: float, s_q: float, s_k: fl
     dev = qkv.get_device()
     rows, P = (0, 0) if table is None else _dims(table, 3, "table")[:2]
     sq, sk = (B, Hq, L, d), (B, Hkv, L, d)
+    new = qkv.new_empty if stream is None else lambda shape: _empty(stream, shape, i8, qkv.device)
     if q is None:
-        q = qkv.new_empty(sq)
+        q = new(sq)
     if k is None:
-        k = qkv.new_empty(sk)
+        k = new(sk)
     if v is None:
-        v = qkv.new_empty(sk)
+        v = new(sk)
     try:
         fits = (qkv.dtype is i8 and qkv.is_contiguous() and dev >= 0
                 and (table is None or table.dtype is i16 and table.shape == (rows, P, 2)
@@ -656,7 +669,7 @@ def requant_heads_int8(q, s_in: float, s_out: float, zp_out: int, bits: int = 8,
     B, H, L, d = _dims(q, 4, "q")
     dev = q.get_device()
     if y is None:
-        y = torch.empty((B, L, H * d), dtype=i8, device=q.device)
+        y = _empty(stream, (B, L, H * d), i8, q.device)
     try:
         fits = (q.dtype is i32 and q.is_contiguous() and dev >= 0
                 and y.dtype is i8 and y.shape == (B, L, H * d) and y.is_contiguous()
