@@ -12,7 +12,7 @@ def calls(fq, put):
     with nothing given that it can make."""
     i8, i32, u8, f32 = torch.int8, torch.int32, torch.uint8, torch.float32
     z = lambda *shape, dtype=i8: put(torch.zeros(*shape, dtype=dtype))  # noqa: E731
-    x, w, mul, q = z(4, 8), z(3, 8), z(3, dtype=f32), z(2, 5, 8)
+    x, w, mul, q = z(4, 8), z(3, 8), z(3, dtype=f32), z(2, 5, 32)
     logits, alpha, ones = z(2, 5, 5, dtype=i32), z(8, dtype=u8), z(8, dtype=f32)
     s, zp = put(torch.ones(1, dtype=torch.float64)), z(1, dtype=i32)
     return [
