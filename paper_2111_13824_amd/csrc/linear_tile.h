@@ -183,6 +183,15 @@ __device__ __forceinline__ void arrive() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// What lanes of this wavefront wrote to LDS before, its other lanes read after, and
+// what they read before is not yet overwritten.  LDS serves a wavefront's accesses
+// in their order; this holds the compiler to it and is no instruction.
+__device__ __forceinline__ void exchange() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // A matrix's rows from `row0` on as a buffer of at most kNone bytes (a tile's are
 // 10 MiB at most): reads beyond its end give nothing.
 constexpr unsigned kNone = 0x70000000u;
@@ -471,6 +480,7 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
                     const int at = 4 * (q0 + q);
                     *reinterpret_cast<vi4*>(mine + 32 * q) = vi4{c[at], c[at + 1], c[at + 2], c[at + 3]};
                 }
+                exchange();
                 const int n = n0 + wn + 32 * f + 8 * q0 + 4 * punit;
 #pragma unroll
                 for (int i = 0; i < kPasses; ++i) {
@@ -483,6 +493,7 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
                     else
                         store_end(o, v, p.N - n);
                 }
+                exchange();
             }
     } else {
         const Epilogue e = epilogue(p);
@@ -512,6 +523,7 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
                 for (int i = 0; i < kPasses; ++i)
                     if (has(i))
                         *reinterpret_cast<vi4*>(const_cast<int8_t*>(part_of) + i * kRows * kPitch) = r[i];
+                exchange();
             }
 #pragma unroll
             for (int f = 0; f < FN; ++f) {
@@ -540,6 +552,7 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
                 const auto z = __builtin_amdgcn_permlane32_swap(d[1], d[3], false, false);
                 *reinterpret_cast<vi4*>(mine + 32 * f) = vi4{(int)x[0], (int)x[1], (int)z[0], (int)z[1]};
             }
+            exchange();
 #pragma unroll
             for (int i = 0; i < kPasses; ++i) {
                 const vi4 v = *reinterpret_cast<const vi4*>(part_of + i * kRows * kPitch);
@@ -555,6 +568,7 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
                 else
                     store_end(y, v, p.N - n);
             }
+            exchange();
         }
     }
 }
