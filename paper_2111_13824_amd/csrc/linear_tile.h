@@ -325,39 +325,12 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
         };
         constexpr int kLoads = S::UN + S::UT;
         const bool ragged = K % STEP != 0;
-        // One stage, its first operands read before: each part's operands are read
-        // under the products of the part before, those of the next stage's first
-        // part, which has arrived by then, under the last.  The stage's own LDS is
-        // free from the barrier on and is filled again.  Where a part is a single
-        // product, too short to read under, all of the next stage's parts are read
-        // under all products of this one, which lie in half `b` of `part` (197 x 1024 x
-        // 1024 4.8 -> 4.4 us, 788 x 768 x 768 4.6 -> 4.3).
-        Part<S> part[2][S::ahead];
-        auto stage = [&](int8_t* cur, int8_t* next, int k, int b) __attribute__((always_inline)) {
-            auto turn = [&]() __attribute__((always_inline)) {
-                arrive<(S::NBUF - 2) * kLoads>();
-                if (ragged && k + 2 == nk) last(next);
-                fill(cur, k + S::NBUF);
-            };
-            if constexpr (S::ahead > 1) {
-                turn();
-#pragma unroll
-                for (int q = 0; q < Q; ++q) part[b ^ 1][q].read(next, q, wa, xa);
-#pragma unroll
-                for (int q = 0; q < Q; ++q) part[b][q].multiply(acc);
-            } else {
-#pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    if (q + 1 < Q) {
-                        part[(q + 1) & 1][0].read(cur, q + 1, wa, xa);
-                    } else {
-                        turn();
-                        part[0][0].read(next, 0, wa, xa);
-                    }
-                    part[q & 1][0].multiply(acc);
-                    interleave<S>();
-                }
-            }
+        // After a stage's last LDS reads: the next one has arrived, and the stage's own
+        // LDS is filled again.
+        auto turn = [&](int8_t* cur, int8_t* next, int k) __attribute__((always_inline)) {
+            arrive<(S::NBUF - 2) * kLoads>();
+            if (ragged && k + 2 == nk) last(next);
+            fill(cur, k + S::NBUF);
         };
 
         // the first stage and the folded bias on their way together, and the other
@@ -368,20 +341,68 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
         if constexpr (S::NBUF == 3) fill(s2, 2);
         arrive<(S::NBUF - 1) * kLoads>();
         if (ragged && nk == 1) last(s0);
-#pragma unroll
-        for (int q = 0; q < S::ahead; ++q) part[0][q].read(s0, q, wa, xa);
-        int8_t* const stages[3] = {s0, s1, s2};
-        // the stages left over come after the loop: a way round them inside it
-        // would have the compiler wait for the youngest load at its head
-        constexpr int kTurn = S::ahead > 1 && S::NBUF % 2 ? 2 * S::NBUF : S::NBUF;
+
+        // The stages left over come after the loops: a way round them inside would have
+        // the compiler wait for the youngest load at the loop's head.
         int k = 0;
-        for (; k + kTurn <= nk; k += kTurn)
+        if constexpr (S::ahead > 1) {
+            // A part is a single product, too short to read under: all of the next
+            // stage's parts are read under all products of this one, which lie in half
+            // `b` of `part` (197 x 1024 x 1024 4.8 -> 4.4 us, 788 x 768 x 768 4.6 -> 4.3).
+            Part<S> part[2][S::ahead];
+            auto stage = [&](int8_t* cur, int8_t* next, int k, int b) __attribute__((always_inline)) {
+                turn(cur, next, k);
 #pragma unroll
-            for (int i = 0; i < kTurn; ++i)
-                stage(stages[i % S::NBUF], stages[(i + 1) % S::NBUF], k + i, i & 1);
+                for (int q = 0; q < Q; ++q) part[b ^ 1][q].read(next, q, wa, xa);
 #pragma unroll
-        for (int i = 0; i + 1 < kTurn; ++i)
-            if (k + i < nk) stage(stages[i % S::NBUF], stages[(i + 1) % S::NBUF], k + i, i & 1);
+                for (int q = 0; q < Q; ++q) part[b][q].multiply(acc);
+            };
+#pragma unroll
+            for (int q = 0; q < Q; ++q) part[0][q].read(s0, q, wa, xa);
+            int8_t* const stages[3] = {s0, s1, s2};
+            constexpr int kTurn = S::NBUF % 2 ? 2 * S::NBUF : S::NBUF;
+            for (; k + kTurn <= nk; k += kTurn)
+#pragma unroll
+                for (int i = 0; i < kTurn; ++i)
+                    stage(stages[i % S::NBUF], stages[(i + 1) % S::NBUF], k + i, i & 1);
+#pragma unroll
+            for (int i = 0; i + 1 < kTurn; ++i)
+                if (k + i < nk) stage(stages[i % S::NBUF], stages[(i + 1) % S::NBUF], k + i, i & 1);
+        } else {
+            // One stage, its first operands read before: each part's operands are read
+            // under the products of the part before, those of the next stage's first
+            // part under the last.  (Written with the loop above, the widest tile spills.)
+            Part<S> part[2];
+            auto stage = [&](int8_t* cur, int8_t* next, int k) __attribute__((always_inline)) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    if (q + 1 < Q) {
+                        part[(q + 1) & 1].read(cur, q + 1, wa, xa);
+                    } else {
+                        turn(cur, next, k);
+                        part[0].read(next, 0, wa, xa);
+                    }
+                    part[q & 1].multiply(acc);
+                    interleave<S>();
+                }
+            };
+            part[0].read(s0, 0, wa, xa);
+            if constexpr (S::NBUF == 3) {
+                for (; k + 3 <= nk; k += 3) {
+                    stage(s0, s1, k);
+                    stage(s1, s2, k + 1);
+                    stage(s2, s0, k + 2);
+                }
+                if (k < nk) stage(s0, s1, k);
+                if (k + 1 < nk) stage(s1, s2, k + 1);
+            } else {
+                for (; k + 2 <= nk; k += 2) {
+                    stage(s0, s1, k);
+                    stage(s1, s0, k + 1);
+                }
+                if (k < nk) stage(s0, s1, k);
+            }
+        }
     } else {
         vi4 a[S::UN], b[S::UT];
         const int8_t *wrow[S::UN], *xrow[S::UT];
@@ -502,8 +523,8 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
             for (int i = t; i < (1 << p.table_bits); i += S::threads) table[i] = p.table[i];
             __syncthreads();
         }
-        const int n = n0 + wn + 16 * punit;
-        const bool whole = n + 16 <= p.N;
+        const int first = n0 + wn + 16 * punit;
+        const bool whole = first + 16 <= p.N;
 #pragma unroll
         for (int g = 0; g < FT; ++g) {
             if constexpr (RES) {
@@ -515,9 +536,9 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
                     r[i] = vi4{0, 0, 0, 0};
                     if (!has(i) || row >= p.T) continue;
                     if (whole)
-                        __builtin_memcpy(&r[i], res + n, 16);
+                        __builtin_memcpy(&r[i], res + first, 16);
                     else
-                        r[i] = load_end(res, p.N, n);
+                        r[i] = load_end(res, p.N, first);
                 }
 #pragma unroll
                 for (int i = 0; i < kPasses; ++i)
@@ -553,6 +574,10 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
                 *reinterpret_cast<vi4*>(mine + 32 * f) = vi4{(int)x[0], (int)x[1], (int)z[0], (int)z[1]};
             }
             exchange();
+            // the place in a row worked out here: kept from the residual's loads on as an
+            // offset of 64 bits and a count, it was spilled in tiles of 256 x 128
+            int n = first;
+            asm volatile("" : "+v"(n));
 #pragma unroll
             for (int i = 0; i < kPasses; ++i) {
                 const vi4 v = *reinterpret_cast<const vi4*>(part_of + i * kRows * kPitch);
