@@ -103,3 +103,36 @@ PRODUCTS = {
     "tile128r": [(2960, 131, 2050), (2050, 301, 2050), (4130, 301, 1001)],
     "tile256r": [(4000, 49, 2050), (3870, 131, 2050), (4130, 65, 2050)],
 }
+
+# Products (T, K, N) of every tile kernel whose rows and channels end on, one before,
+# one after and a unit away from the edges of its tiles, with one stage of inputs
+# to seven, whole and ragged ones.
+EDGES = {
+    "tile64": [(319, 128, 832), (448, 112, 896), (577, 144, 448), (4160, 256, 63), (3328, 384, 65),
+        (2753, 416, 81), (2367, 512, 111), (161, 592, 784), (161, 768, 752), (4160, 896, 31), (1935, 48,
+        193)],
+    "tile128": [(5503, 128, 384), (5504, 112, 384), (2689, 144, 768), (5504, 256, 383), (6656, 384,
+        257), (6529, 416, 273), (8319, 512, 239), (6625, 592, 272), (8225, 768, 240), (8256, 896, 223),
+        (6543, 48, 257)],
+    "tile256x128": [(5503, 64, 768), (5504, 48, 768), (1153, 80, 3328), (5504, 128, 767), (6656, 192,
+        513), (6529, 224, 529), (8319, 256, 495), (6625, 272, 528), (1185, 384, 3312), (8256, 448, 479),
+        (8207, 48, 385)],
+    "tile256x192": [(2495, 128, 3328), (2496, 112, 3328), (5377, 144, 1536), (2496, 256, 3327), (13248,
+        384, 513), (13057, 416, 529), (10943, 512, 751), (13217, 592, 528), (5409, 768, 1520), (11072,
+        896, 735), (10959, 48, 641)],
+    "tile256x256": [(4863, 256, 2560), (4864, 256, 2560), (6913, 256, 1792), (4864, 256, 2559), (16384,
+        384, 513), (16385, 416, 529), (16383, 512, 751), (16353, 592, 528), (6945, 768, 1776), (16576,
+        896, 735), (16399, 256, 641)],
+    "tile256x320": [(13119, 128, 1280), (13120, 112, 1280), (21761, 144, 768), (7680, 256, 2303),
+        (22080, 384, 513), (21761, 416, 529), (9279, 512, 1775), (22049, 592, 528), (6433, 768, 2544),
+        (22016, 896, 735), (21775, 48, 641)],
+    "tile64r": [(319, 129, 832), (320, 127, 832), (385, 259, 640), (3136, 17, 127), (3328, 379, 65),
+        (1409, 520, 81), (2751, 641, 47), (417, 15, 912), (161, 767, 752), (4160, 903, 31), (1935, 33,
+        193)],
+    "tile128r": [(4479, 129, 1408), (4480, 127, 1408), (2689, 259, 1920), (7040, 129, 895), (7296, 379,
+        513), (7041, 520, 401), (8319, 641, 367), (7649, 129, 784), (8225, 767, 368), (8256, 903, 223),
+        (7567, 129, 769)],
+    "tile256r": [(11007, 65, 768), (11008, 63, 768), (5377, 131, 1536), (7424, 17, 1279), (13312, 187,
+        513), (13057, 264, 529), (16639, 321, 495), (16609, 15, 528), (16417, 383, 496), (16576, 455,
+        479), (13583, 33, 641)],
+}

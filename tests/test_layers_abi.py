@@ -110,6 +110,23 @@ def test_products_of_the_gpu_tests_reach_every_kernel(lib):
         assert R.KERNELS[lib.fq_test_linear_kernel()] == "tile64r"
 
 
+def test_edges_of_the_gpu_tests_are_those_of_the_tiles(lib):
+    """Each product of EDGES takes its kernel, and each kernel's reach the edges of its
+    tiles: rows and channels of whole tiles, one less and one more."""
+    import layer_cases as R
+    assert set(R.EDGES) == set(R.KERNELS) - {"rows16", "rows32"}
+    call = caller(lib, "linear_int32", x=16, T=1, w=16, N=1, K=1, fold=None, out=1)
+    for name, products in R.EDGES.items():
+        bn, bt, _ = WORKGROUPS[name]
+        for T, K, N in products:
+            assert call(T=T, K=K, N=N) == RAN
+            assert R.KERNELS[lib.fq_test_linear_kernel()] == name, (name, T, K, N)
+        assert {T % bt for T, _, _ in products} >= {0, 1, bt - 1}, name
+        assert {N % bn for _, _, N in products} >= {0, 1, bn - 1}, name
+        # ends inside a unit of 16, and on one
+        assert {N % 16 for _, _, N in products} >= {0, 1, 15}, name
+
+
 # channels, rows and threads of a workgroup
 WORKGROUPS = dict(rows16=(16, 16, 512), rows32=(16, 32, 512), tile64=(64, 64, 256), tile128=(128, 128, 256),
                   tile256x128=(256, 128, 512), tile256x192=(256, 192, 512), tile256x256=(256, 256, 512),
