@@ -84,21 +84,41 @@ int cheapest(const LinearArgs& a, const Cost (&costs)[shapes]) {
 
 inline int64_t ceil_div(int64_t a, int b) { return (a + b - 1) / b; }
 
+// Up to 32 rows the tiles are one line of them, and their time is the weights' way to
+// the chip: fixed + K (input + tile times the number of tiles of 64 x 64), in
+// microseconds, fitted to products of weights that come from HBM (K 192 .. 4096, N 1024
+// .. 65536).  The kernels of few rows reach memory sooner, but their rounds cost more
+// than their weights once there are several: K = 1024, 16 and 32 rows: 3.6 and 4.0 us for
+// N = 4096 (tiles 4.9), 5.6 and 7.2 for 12288 (6.3), 11.4 and 16.5 for 32768 (9.4).
+// Up to 8 rows they keep up with the tiles for most N (2 rows of K = 1024, N = 65536: 15.9
+// us, tiles 18.3).  Fitted to 402 products of 1 to 32 rows (1.1% over the fastest kernel of
+// each, 24% at most); on 103 others (K to 20000, N to 120000) 2.4% over it, where the
+// kernels of few rows alone took 15% more, and 2.4 times as long at most.
+struct LineCost {
+    float fixed, input, tile;
+};
+constexpr LineCost kLine[2] = {{3.6f, 6.6e-3f, 1.95e-5f}, {4.1f, 2.06e-3f, 1.66e-6f}};   // whole units
+
 // Rows of whole 16-byte units on 16-byte aligned bases can be loaded straight into
 // LDS.
 inline Kernel plan(const LinearArgs& a) {
-    if (a.T <= 16) return kRows16;
     const bool units = a.K % 16 == 0 &&
                        ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15) == 0;
-    if (a.T <= 32 || ceil_div(a.T, 64) * ceil_div(a.N, 64) <= 256) {
+    if (a.T <= 8) return kRows16;
+    const int64_t tiles = ceil_div(a.T, 64) * ceil_div(a.N, 64);
+    if (a.T <= 32 || tiles <= 256) {
         float cost[3];
         for (int i = 0; i < 3; ++i) {
             const FewCost& c = kFew[units][i];
             const int64_t blocks = i < 2 ? ceil_div(a.N, 16) * ceil_div(a.T, 16 << i) : 1;
             cost[i] = c.fixed + (float)ceil_div(blocks, 256) * (c.round + c.input * (float)a.K);
         }
-        if (a.T <= 32 || cost[0] < cost[2] || cost[1] < cost[2])
-            return cost[0] < cost[1] ? kRows16 : kRows32;
+        const LineCost& l = kLine[units];
+        if (a.T <= 32) cost[2] = l.fixed + (float)a.K * (l.input + l.tile * (float)tiles);
+        if (cost[0] < cost[2] || cost[1] < cost[2]) return cost[0] < cost[1] ? kRows16 : kRows32;
+        // most rows of a larger tile would be empty (16 rows of K = 464, N = 93454: 16.2 us,
+        // 19.4 in 128 x 128; 17 of K = 1001, N = 65537: 27.1 and 33.5)
+        if (a.T <= 32) return units ? kTile64 : kTile64R;
     }
     return units ? (Kernel)(kTile64 + cheapest(a, kCosts))
                  : (Kernel)(kTile64R + cheapest(a, kCostsR));

@@ -136,3 +136,7 @@ EDGES = {
         513), (13057, 264, 529), (16639, 321, 495), (16609, 15, 528), (16417, 383, 496), (16576, 455,
         479), (13583, 33, 641)],
 }
+
+# Products (T, K, N) of 9 to 32 rows whose channels are many: one line of tiles.
+WIDE = [(9, 1024, 40000), (16, 272, 45001), (17, 768, 16384), (31, 272, 33017), (32, 1024, 32768),
+        (10, 301, 50001), (16, 500, 50001), (17, 1001, 16385), (32, 129, 33000)]

@@ -110,6 +110,32 @@ def test_products_of_the_gpu_tests_reach_every_kernel(lib):
         assert R.KERNELS[lib.fq_test_linear_kernel()] == "tile64r"
 
 
+def test_wide_products_of_few_rows_take_tiles(lib):
+    """9 to 32 rows of products whose channels come to several workgroups of few rows a CU
+    take one line of tiles (32 x 1024 x 32768: 9.5 us, 16.5 in the kernel of 32 rows); narrow
+    ones, and up to 8 rows all, do not."""
+    import layer_cases as R
+    call = caller(lib, "linear_int8", x=16, T=1, w=16, N=1, K=1, fold=None, mul=16, act=0, table=None,
+                  tbits=0, zp_t=0, res=None, zp_r=0, mul_r=1.0, zp=0, bits=8, y=1)
+
+    def kernel(T, K, N):
+        assert call(T=T, K=K, N=N) == RAN
+        return R.KERNELS[lib.fq_test_linear_kernel()]
+
+    for T, K, N in R.WIDE:
+        assert kernel(T, K, N) == ("tile64" if K % 16 == 0 else "tile64r"), (T, K, N)
+    for T in (17, 24, 32):
+        for K in (768, 1024, 2048, 4096):
+            for N in (1024, 4096, 8192):
+                assert kernel(T, K, N) in ("rows16", "rows32"), (T, K, N)
+            for N in (16384, 32768, 65536):
+                assert kernel(T, K, N) == "tile64", (T, K, N)
+            assert kernel(T, K + 1, 32769) == "tile64r"
+    for T in (1, 2, 8):
+        for N in (1, 4096, 65536, 1 << 20):
+            assert kernel(T, 1024, N) == kernel(T, 1001, N) == "rows16"
+
+
 def test_edges_of_the_gpu_tests_are_those_of_the_tiles(lib):
     """Each product of EDGES takes its kernel, and each kernel's reach the edges of its
     tiles: rows and channels of whole tiles, one less and one more."""

@@ -51,6 +51,22 @@ def test_edges_of_every_tile(fq, name, T, K, N):  # noqa: F811
     assert intact()
 
 
+@pytest.mark.parametrize("T,K,N", R.WIDE)
+def test_wide_products_of_few_rows(fq, T, K, N):  # noqa: F811
+    """One line of tiles, most of whose rows are not there: every epilogue."""
+    say("wide", T, K, N)
+    p = R.layer(T, K, N, seed=T, zp_x=4)
+    f, m = R.fold(p["w"], p["s_w"], p["s_x"], p["s_y"], 4, p["bias"])
+    r = np.random.default_rng(N).integers(-128, 128, (T, N)).astype(np.int8)
+    table = np.random.default_rng(T).normal(0, 60, 256).astype(np.float32)
+    for kw in ({}, dict(relu=True), dict(table=table, zp_t=128)):
+        check(fq, T, p["x"], p["w"], f, m, zp_y=-9, **kw)
+        check(fq, T, p["x"], p["w"], f, m, zp_y=-9, residual=r, zp_r=3, mul_r=0.7, **kw)
+    out, intact = guarded((T, N), dev(f).dtype, 4)
+    fq.linear_int32(dev(p["x"]), dev(p["w"]), dev(f), out=out)
+    assert np.array_equal(host(out), R.sums(p["x"], p["w"], f)) and intact()
+
+
 @pytest.mark.parametrize("name", R.KERNELS)
 @pytest.mark.parametrize("mul,zp", [(0.5, 1), (0.25, -7)])
 def test_ties_go_to_the_even_neighbour_in_every_kernel(fq, name, mul, zp):  # noqa: F811
