@@ -151,7 +151,7 @@ def _check(fn: str, status: int) -> None:
 
 def _narrow(name: str, args) -> None:
     """Raises where ctypes would silently drop the high bits of an integer (a
-    row of 2^32 + 16 values would be taken for one of 16).  0.2 us a call."""
+    row of 2^32 + 16 values would be taken for one of 16)."""
     ints, pack = _INT32S[name]
     try:
         pack(*ints(args))
@@ -202,7 +202,11 @@ def _invoke(name: str, args, keep, prepare: bool, result, device: Optional[int] 
     """Run the entry point now, or return it prepared for repeated calls."""
     if prepare:
         return Prepared(name, args, keep, device)
-    _narrow(name, args)
+    try:                       # as _narrow, without a call more on the way of each call
+        ints, pack = _INT32S[name]
+        pack(*ints(args))
+    except struct.error:
+        _narrow(name, args)
     st = _enter(getattr(_lib or lib(), name), args, device)
     if st != FQ_OK:
         raise FqError(name, st)
@@ -248,16 +252,17 @@ def _raw_stream(stream, device: int) -> int:
     return torch._C._cuda_getCurrentRawStream(device)
 
 
-def _empty(stream, shape, dtype, device):
-    """An output or workspace that the caller did not give, from the memory of the
-    stream that the call runs on: torch's allocator then hands it on only behind
-    that stream's work (memory of the current stream could still be in use there
-    when another stream writes it, or be handed on while that stream still does)."""
-    import torch
+def _empty(like, stream, shape, dtype):
+    """An output or workspace that the caller did not give, on the device of `like`
+    and from the memory of the stream that the call runs on: torch's allocator
+    then hands it on only behind that stream's work (memory of the current stream
+    could still be in use there when another stream writes it, or be handed on
+    while that stream still does)."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
+    import torch
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(shape, dtype=dtype, device=like.device)
 
 
 def ptf_layernorm_int8(x_q, zp_in: int, alpha, K: int, gamma, beta, s_out: float, zp_out: int,
@@ -267,7 +272,7 @@ def ptf_layernorm_int8(x_q, zp_in: int, alpha, K: int, gamma, beta, s_out: float
     import torch
     T, C = x_q.shape
     if y_q is None:
-        y_q = _empty(stream, x_q.shape, x_q.dtype, x_q.device)
+        y_q = torch.empty_like(x_q) if stream is None else _empty(x_q, stream, x_q.shape, torch.int8)
     if alpha.shape != (C,) or gamma.shape != (C,) or beta.shape != (C,) or y_q.shape != (T, C):
         raise ValueError("alpha, gamma, beta must be [C] and y_q [T, C]")
     args = (_dev_ptr(x_q, torch.int8, "x_q", 2), T, C, zp_in,
@@ -292,7 +297,7 @@ def lis_softmax_log4(logits, s_logit: float, bits: int = 4, exp_n: int = 20, bia
     if codes is None:
         # rows without padding: the kernel writes every byte (an odd row's last
         # high nibble 0)
-        codes = _empty(stream, (G, Lq, codes_ld(Lk, bits)), torch.uint8, logits.device)
+        codes = _empty(logits, stream, (G, Lq, codes_ld(Lk, bits)), torch.uint8)
     if codes.dim() != 3 or codes.shape[:2] != (G, Lq):
         raise ValueError("codes must be [G, Lq, ld_codes]")
     Hb = 0
@@ -315,7 +320,7 @@ def lis_attn_v_shift(codes, v, Lk: int, zp_v: int = 0, bits: int = 4, out=None, 
     if v.dim() != 3 or v.shape[:2] != (G, Lk):
         raise ValueError("v must be [G, Lk, d]")
     if out is None:
-        out = _empty(stream, (G, Lq, d), torch.int32, v.device)
+        out = _empty(v, stream, (G, Lq, d), torch.int32)
     if out.shape != (G, Lq, d):
         raise ValueError("out must be [G, Lq, d]")
     args = (_dev_ptr(codes, torch.uint8, "codes", 3), ld, _dev_ptr(v, torch.int8, "v", 3), zp_v,
@@ -333,7 +338,7 @@ def lis_attn_v_shift_wide(codes, v, Lk: int, zp_v: int = 0, bits: int = 8, out=N
     if v.dim() != 3 or v.shape[:2] != (G, Lk):
         raise ValueError("v must be [G, Lk, d]")
     if out is None:
-        out = _empty(stream, (G, Lq, d), torch.int64, v.device)
+        out = _empty(v, stream, (G, Lq, d), torch.int64)
     if out.shape != (G, Lq, d):
         raise ValueError("out must be [G, Lq, d]")
     args = (_dev_ptr(codes, torch.uint8, "codes", 3), ld, _dev_ptr(v, torch.int8, "v", 3), zp_v,
@@ -350,7 +355,7 @@ def lis_attention_head(logits, v, s_logit: float, bits: int = 4, exp_n: int = 20
     if v.dim() != 3 or v.shape[:2] != (G, Lk):
         raise ValueError("v must be [G, Lk, d]")
     if out is None:
-        out = _empty(stream, (G, Lq, d), torch.int32, logits.device)
+        out = _empty(logits, stream, (G, Lq, d), torch.int32)
     if out.shape != (G, Lq, d):
         raise ValueError("out must be [G, Lq, d]")
     Hb = 0
@@ -382,13 +387,12 @@ def ptf_calibrate(x, bits: int = 8, K: int = 3, s=None, zp=None, alpha=None, wor
     workspace is allocated here with torch when not given."""
     import torch
     T, C = x.shape
-    dev = x.device
-    s = _empty(stream, 1, torch.float64, dev) if s is None else s
-    zp = _empty(stream, 1, torch.int32, dev) if zp is None else zp
-    alpha = _empty(stream, C, torch.uint8, dev) if alpha is None else alpha
+    s = _empty(x, stream, 1, torch.float64) if s is None else s
+    zp = _empty(x, stream, 1, torch.int32) if zp is None else zp
+    alpha = _empty(x, stream, C, torch.uint8) if alpha is None else alpha
     need = ptf_calibrate_workspace_bytes(T, C, K) if T > 0 else 0
     if workspace is None:
-        workspace = _empty(stream, max(need, 1), torch.uint8, dev)
+        workspace = _empty(x, stream, max(need, 1), torch.uint8)
     args = (_dev_ptr(x, torch.float32, "x", 2), T, C, bits, K,
             _dev_ptr(s, torch.float64, "s", 1), _dev_ptr(zp, torch.int32, "zp", 1),
             _dev_ptr(alpha, torch.uint8, "alpha", 1), _dev_ptr(workspace, torch.uint8, "workspace", 1),
@@ -403,10 +407,9 @@ def ptf_calibrate_noalloc(x, bits: int = 8, K: int = 3, s=None, zp=None, alpha=N
     by torch, before the call)."""
     import torch
     T, C = x.shape
-    dev = x.device
-    s = _empty(stream, 1, torch.float64, dev) if s is None else s
-    zp = _empty(stream, 1, torch.int32, dev) if zp is None else zp
-    alpha = _empty(stream, C, torch.uint8, dev) if alpha is None else alpha
+    s = _empty(x, stream, 1, torch.float64) if s is None else s
+    zp = _empty(x, stream, 1, torch.int32) if zp is None else zp
+    alpha = _empty(x, stream, C, torch.uint8) if alpha is None else alpha
     args = (_dev_ptr(x, torch.float32, "x", 2), T, C, bits, K,
             _dev_ptr(s, torch.float64, "s", 1), _dev_ptr(zp, torch.int32, "zp", 1),
             _dev_ptr(alpha, torch.uint8, "alpha", 1), _stream(stream, x))
@@ -420,7 +423,7 @@ def ptf_quantize_int8(x, s, zp, alpha, bits: int = 8, x_q=None, stream=None,
     import torch
     T, C = x.shape
     if x_q is None:
-        x_q = _empty(stream, (T, C), torch.int8, x.device)
+        x_q = _empty(x, stream, (T, C), torch.int8)
     if alpha.shape != (C,) or x_q.shape != (T, C):
         raise ValueError("alpha must be [C] and x_q [T, C]")
     args = (_dev_ptr(x, torch.float32, "x", 2), T, C, _dev_ptr(s, torch.float64, "s", 1),
@@ -435,7 +438,7 @@ def requant_dyadic_int8(q, s_in: float, s_out: float, zp_out: int, bits: int = 8
     int8 container; returns (or fills) int8 of the same shape."""
     import torch
     if y is None:
-        y = _empty(stream, q.shape, torch.int8, q.device)
+        y = _empty(q, stream, q.shape, torch.int8)
     if y.shape != q.shape:
         raise ValueError("y must have the shape of q")
     args = (_dev_ptr(q, torch.int32, "q"), q.numel(), s_in, s_out, zp_out, bits,
@@ -455,7 +458,7 @@ def lis_attention_qk(q, k, v, s_logit: float, zp_q: int = 0, zp_k: int = 0, bits
     if k.shape != (G, Lk, dk) or v.shape[:2] != (G, Lk):
         raise ValueError("k must be [G, Lk, dk] and v [G, Lk, d]")
     if out is None:
-        out = _empty(stream, (G, Lq, d), torch.int32, q.device)
+        out = _empty(q, stream, (G, Lq, d), torch.int32)
     Hb = bias.shape[0] if bias is not None else 0
     args = (_dev_ptr(q, torch.int8, "q", 3), _dev_ptr(k, torch.int8, "k", 3), zp_q, zp_k, dk,
             _dev_ptr(bias, torch.int32, "bias", 3), Hb, G, Lq, Lk, s_logit, bits, exp_n,
@@ -475,9 +478,9 @@ def linear_fold_int8(w, s_w, s_x: float, s_y: float = 1.0, zp_x: int = 0, bias=N
     N, K = _dims(w, 2, "w")
     dev = w.get_device()
     if fold is None:
-        fold = _empty(stream, N, torch.int32, w.device)
+        fold = _empty(w, stream, N, torch.int32)
     if mul is None:
-        mul = _empty(stream, N, torch.float32, w.device)
+        mul = _empty(w, stream, N, torch.float32)
     specs = [("w", w, torch.int8, (N, K)), ("s_w", s_w, torch.float32, (N,)),
              ("fold", fold, torch.int32, (N,)), ("mul", mul, torch.float32, (N,))]
     if bias is not None:
@@ -517,7 +520,7 @@ def linear_int8(x, w, fold, mul, zp_y: int = 0, bits: int = 8, relu: bool = Fals
     elif relu:
         act = ACT_RELU
     if y is None:
-        y = x.new_empty((T, N)) if stream is None else _empty(stream, (T, N), i8, x.device)
+        y = x.new_empty((T, N)) if stream is None else _empty(x, stream, (T, N), i8)
     try:
         fits = (x.dtype is i8 and x.is_contiguous() and dev >= 0
                 and w.dtype is i8 and w.shape == (N, K) and w.is_contiguous()
@@ -554,7 +557,7 @@ def linear_int32(x, w, fold=None, out=None, stream=None, prepare: bool = False):
     N = w.shape[0]
     dev = x.get_device()
     if out is None:
-        out = _empty(stream, (T, N), i32, x.device)
+        out = _empty(x, stream, (T, N), i32)
     try:
         fits = (x.dtype is i8 and x.is_contiguous() and dev >= 0
                 and w.dtype is i8 and w.shape == (N, K) and w.is_contiguous()
@@ -600,7 +603,7 @@ def rope_table_int16(positions, freq, axis, table=None, stream=None, prepare: bo
     P, = _dims(freq, 1, "freq")
     dev = positions.get_device()
     if table is None:
-        table = _empty(stream, (T, P, 2), i16, positions.device)
+        table = _empty(positions, stream, (T, P, 2), i16)
     try:
         fits = (positions.dtype is i32 and positions.is_contiguous() and dev >= 0
                 and freq.dtype is f64 and freq.is_contiguous() and freq.get_device() == dev
@@ -634,7 +637,7 @@ def rope_qkv_int8(qkv, table, Hq: int, Hkv: int, s_x: float, s_q: float, s_k: fl
     dev = qkv.get_device()
     rows, P = (0, 0) if table is None else _dims(table, 3, "table")[:2]
     sq, sk = (B, Hq, L, d), (B, Hkv, L, d)
-    new = qkv.new_empty if stream is None else lambda shape: _empty(stream, shape, i8, qkv.device)
+    new = qkv.new_empty if stream is None else lambda shape: _empty(qkv, stream, shape, i8)
     if q is None:
         q = new(sq)
     if k is None:
@@ -669,7 +672,7 @@ def requant_heads_int8(q, s_in: float, s_out: float, zp_out: int, bits: int = 8,
     B, H, L, d = _dims(q, 4, "q")
     dev = q.get_device()
     if y is None:
-        y = _empty(stream, (B, L, H * d), i8, q.device)
+        y = _empty(q, stream, (B, L, H * d), i8)
     try:
         fits = (q.dtype is i32 and q.is_contiguous() and dev >= 0
                 and y.dtype is i8 and y.shape == (B, L, H * d) and y.is_contiguous()
