@@ -388,13 +388,13 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
             };
             part[0].read(s0, 0, wa, xa);
             if constexpr (S::NBUF == 3) {
-                for (; k + 3 <= nk; k += 3) {
-                    stage(s0, s1, k);
-                    stage(s1, s2, k + 1);
-                    stage(s2, s0, k + 2);
-                }
-                if (k < nk) stage(s0, s1, k);
-                if (k + 1 < nk) stage(s1, s2, k + 1);
+                int8_t* const stages[3] = {s0, s1, s2};
+                for (; k + 3 <= nk; k += 3)
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) stage(stages[i], stages[(i + 1) % 3], k + i);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (k + i < nk) stage(stages[i], stages[i + 1], k + i);
             } else {
                 for (; k + 2 <= nk; k += 2) {
                     stage(s0, s1, k);
@@ -574,10 +574,10 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
                 *reinterpret_cast<vi4*>(mine + 32 * f) = vi4{(int)x[0], (int)x[1], (int)z[0], (int)z[1]};
             }
             exchange();
-            // the place in a row worked out here: kept from the residual's loads on as an
-            // offset of 64 bits and a count, it was spilled in tiles of 256 x 128
+            // with a residual, the place in a row worked out here: kept from the residual's
+            // loads on as an offset of 64 bits and a count, it was spilled in tiles of 256 x 128
             int n = first;
-            asm volatile("" : "+v"(n));
+            if constexpr (RES) asm volatile("" : "+v"(n));
 #pragma unroll
             for (int i = 0; i < kPasses; ++i) {
                 const vi4 v = *reinterpret_cast<const vi4*>(part_of + i * kRows * kPitch);
