@@ -324,7 +324,7 @@ fq_status requant_dyadic_int8(const int32_t* q, int64_t n, float s_in, float s_o
  * A channel whose s_w[n] is not positive and finite takes mul[n] = 0 and no
  * bias; a bias that is not a number counts as 0.
  *
- *   w      [N, K] int8, N in [1, 2^20], K in [1, 32768].
+ *   w      [N, K] int8 of any alignment, N in [1, 2^20], K in [1, 32768].
  *   s_w    [N] float; bias [N] float or NULL (none).
  *   zp_x   in [-128, 127]; s_x, s_y positive and finite.  s_y is the output's
  *          step, or the step of the activation's input where a table follows.
@@ -355,8 +355,8 @@ fq_status linear_fold_int8(const int8_t* w, int32_t N, int32_t K, const float* s
  *   y      [T, N] int8 container (out).  It may be the residual itself; it
  *          overlaps no other argument.
  * T >= 0, N in [1, 2^20], K in [1, 32768], fewer than 2^24 tiles of 64 x 64
- * outputs.  Bases of any alignment; rows of whole 16-byte units on 16-byte aligned
- * bases take the fast path.
+ * outputs.  int8 bases of any alignment, int32 and float ones of 4 bytes; rows of x
+ * and w of whole 16-byte units on 16-byte aligned bases take the fast path.
  *
  * With acc = sum_k x[t,k] w[n,k] + fold[n] exact in int32, RN = rounding to the
  * nearest binary32 and rint = to the nearest integer (ties to even in both), of
@@ -419,8 +419,8 @@ fq_status fq_activation_table(int32_t kind, float s_t, int32_t zp_t, int32_t tab
  * the middle of two integers.  Position 0 gives (2^14, 0): no turn at all.
  *
  *   positions  [axes, T] int32, axes in [1, 8], T in [0, 2^25].
- *   freq   [P] double (finite), P in [1, 128]; axis [P] uint8 (values at or
- *          above `axes` are taken as axes - 1).
+ *   freq   [P] double, P in [1, 128], its products with the positions finite;
+ *          axis [P] uint8 (values at or above `axes` are taken as axes - 1).
  *   table  [T, P, 2] int16 (out), 4-byte aligned.
  * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (T, axes, P), FQ_ERR_PARAM (table not
  * aligned).
@@ -462,7 +462,8 @@ fq_status rope_qkv_int8(const int8_t* qkv, int64_t B, int32_t L, int32_t Hq, int
  * requant_dyadic_int8 of an attention result, with its heads brought back to
  * rows: q [B, H, L, d] int32 (lis_attention_qk's out) -> y [B, L, H d] int8, as
  * the projection's linear layer reads it.  The same dyadic multiplier and
- * rounding; B L in [0, 2^25], H in [1, 1024], d in [1, 256].
+ * rounding; B L in [0, 2^25], H in [1, 1024], d in [1, 256]; q 4-byte aligned, y
+ * of any alignment.
  * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (B or L < 0, H, d), FQ_ERR_PARAM (bits, a
  * scale or zp_out out of range).
  */

@@ -2,8 +2,9 @@
 // heads back to rows, for gfx950.  Both move each byte once and are bound by
 // memory: what counts is that rows are read and written in whole lines with many
 // loads under way.  On ViT-L/16 at batch 16 (9232 rows of 48 heads of 64, 57 MB) the
-// rotation takes 12.0 us, 4.7 TB/s; on ViT-B/16 at batch 64 the way back to rows
-// (48 MB) 9.2 us, 5.2 TB/s; a large copy reaches 5.1.
+// rotation takes 13.4 us by itself (median of a trace; 11.6 at least), 12.6 among
+// others of its kind, 4.5 TB/s; on ViT-B/16 at batch 64 the way back to rows (48 MB)
+// 11.2 (9.8) and 10.6, 4.6 TB/s; a large copy reaches 5.1.
 #include <algorithm>
 
 #include "bytes_device.h"

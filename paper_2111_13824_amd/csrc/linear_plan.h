@@ -41,8 +41,9 @@ constexpr FewCost kFew[2][3] = {    // 16 rows, 32 rows, a round of tiles of 64 
 // share a CU; a CU's tiles take per round of `per` fixed + input K microseconds, the
 // share `few` of it at least.  Large tiles move fewer bytes through L2 for a product
 // but fill the last round worse:
-// 9232 x 1024 x 4096 takes 45 us in 464 tiles of 256 x 320 and 53 in 592 of 256 x 256;
-// 9232 x 4096 x 1024 takes 40 us in 196 tiles of 256 x 192 and 44 in 148 of 256 x 256;
+// 9232 x 1024 x 4096 takes 45 us in 464 tiles of 256 x 320 and 53 in 592 of 256 x 256
+// (48 with a table, which the fit leaves out, as it does residuals); 9232 x 4096 x 1024
+// takes 40 us in 196 tiles of 256 x 192 and 44 in 148 of 256 x 256 (42 with a residual);
 // 12608 x 768 x 2304 takes 30 us in 450 tiles of 256 x 256 and 34 in 360 of 256 x 320;
 // 788 x 768 x 768 takes 4.3 us in 156 tiles of 64 x 64 and 13 in 12 of 256 x 256.
 // Over the 136 the choice costs 0.05% more than the fastest tile of each.

@@ -461,8 +461,8 @@ __global__ __launch_bounds__(S::threads, S::waves) void linear_tile_kernel(Linea
 
     // Epilogue.  Lane (row, h) of a block holds channels 8 q + 4 h + 0 .. 3 of its
     // row, q = 0 .. 3.  A wavefront brings 32 rows at a time through LDS of its
-    // own, so that its stores (and the residual's loads) are whole runs of the
-    // rows: 128 bytes where FN = 4, instead of 32.
+    // own, so that its stores (and the residual's loads) are runs of the rows of 32
+    // FN bytes in whole 16-byte units: 64 where FN = 2, half a line.
     vf4 mul[FN][4];
     if constexpr (!ACC) {
         const __amdgpu_buffer_rsrc_t mr =
