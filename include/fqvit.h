@@ -2,8 +2,9 @@
  * fqvit.h -- C ABI of the MI355X (gfx950) library for the integer hot path of
  * FQ-ViT (Lin et al., "FQ-ViT: Post-Training Quantization for Fully Quantized
  * Vision Transformer", IJCAI 2022): Power-of-Two-Factor LayerNorm and
- * Log-Int-Softmax attention, and the linear layers, rotary positions and
- * requantization around them.
+ * Log-Int-Softmax attention, the linear layers, rotary positions and
+ * requantization around them, and the step over a stream of tokens: root-mean-square
+ * norm, paged cache, attention over it, eviction from it.
  *
  * Conventions shared by every entry point
  *   - Tensor arguments are DEVICE pointers into memory the caller owns (for
@@ -19,8 +20,9 @@
  *   - Every argument is validated on the host before anything is enqueued.  A
  *     failing check returns its status code and enqueues nothing.  Empty
  *     tensors (T, G or Lq equal to 0) return FQ_OK and enqueue nothing.
- *   - Integer outputs are a pure function of the arguments (no atomics, no
- *     order dependence): the same call gives the same bits every time.
+ *   - Integer outputs are a pure function of the arguments (no order
+ *     dependence; atomics, where there are any, add integers): the same call
+ *     gives the same bits every time.
  *   - Quantized activations live on the paper's unsigned b-bit grid
  *     {0 .. 2^b - 1} (Sec. 3.1, eq. 2).  The int8 containers used here hold
  *     (paper value - 2^(b-1)); zero points are shifted the same way.  Every
@@ -60,7 +62,8 @@ int32_t fq_version(void);
  * semantics), so hipEventElapsedTime gives the kernel's own duration with no
  * extra packets on the stream.  Every other entry point launches one kernel.
  * ptf_calibrate, which launches four kernels, records `start` on the first and
- * `stop` on the last, so the interval covers the whole calibration.
+ * `stop` on the last, so the interval covers the whole calibration; so do
+ * lis_attention_paged and kv_cache_evict where they launch several.
  * The events are consumed by that next call whatever it returns; a call that
  * enqueues nothing (empty tensors, failed validation) leaves them unrecorded.
  * Always returns FQ_OK.
@@ -470,6 +473,139 @@ fq_status rope_qkv_int8(const int8_t* qkv, int64_t B, int32_t L, int32_t Hq, int
 fq_status requant_heads_int8(const int32_t* q, int64_t B, int32_t H, int32_t L, int32_t d,
                              float s_in, float s_out, int32_t zp_out, int32_t bits, int8_t* y,
                              void* stream);
+
+/*
+ * Root-mean-square norm of a stream of tokens with the addition of a branch: the
+ * LayerNorm's integer form (Supplement A.1: exact sums of integers, one normaliser a
+ * row) without the mean, for layers whose residual stream is kept in 16 bits.
+ *
+ *   x      NULL (no branch) or [T, C] int8 container of the branch, zero point zp_x in
+ *          [-128, 127]; alpha NULL (zeros) or [C] uint8 power-of-two factors (Sec.
+ *          3.2), values above K (0..7) are clamped to K.  m_x = s_x / s_r, the steps of
+ *          branch and stream, in [2^-20, 64].
+ *   r      [T, C] int16, the stream (zero point 0).
+ *   gamma  [C] float, finite.  eps >= 0, finite: the norm's epsilon in steps of the
+ *          stream, eps_real / s_r^2.
+ *   h      [T, C] int16 (out): the stream with the branch; it may be r itself.
+ *   y      [T, C] int8 container (out) of the b-bit grid, b in [2, 8].
+ * T in [0, 2^24 - 1], C in [1, 8192]; other overlaps are not allowed.  With RN =
+ * rounding to the nearest binary32 and rint = to the nearest integer (ties to even in
+ * both) of the exact value, RN64 likewise to binary64:
+ *   h = clip(r + rint((x - zp_x) 2^min(alpha, K) m_x), -32768, 32767)
+ *   M2 = sum_c h^2, exact;  D = RN64(RN64(M2 / C) + eps)
+ *   rho = RN64(1 / RN64(sqrt D)), 0 where D = 0
+ * rmsnorm_int8, with a scale s_out (positive, finite) and zero point zp_out:
+ *   y = clip(rint(h RN(gamma RN(RN64(rho / s_out))) + zp_out))
+ * rmsnorm_rows_int8, with a scale for each row, scales [T] float (out), t = 2^(b-1) - 1:
+ *   a = RN(gamma h), A = max_c |a|
+ *   y = rint(a RN(RN64(t / A))), all 0 where A = 0;  scales = RN(RN(A RN(rho)) / t)
+ * (a value that leaves binary32 on the way gives an unspecified y.)
+ * Errors: FQ_ERR_NULL (r, gamma, h, y; scales), FQ_ERR_SHAPE (T, C), FQ_ERR_PARAM (bits,
+ * K, zero points, m_x, eps, s_out; what is not used is not looked at).
+ */
+fq_status rmsnorm_int8(const int8_t* x, int32_t zp_x, const uint8_t* alpha, int32_t K, float m_x,
+                       const int16_t* r, int64_t T, int32_t C, const float* gamma, float eps,
+                       float s_out, int32_t zp_out, int32_t bits, int16_t* h, int8_t* y,
+                       void* stream);
+fq_status rmsnorm_rows_int8(const int8_t* x, int32_t zp_x, const uint8_t* alpha, int32_t K,
+                            float m_x, const int16_t* r, int64_t T, int32_t C, const float* gamma,
+                            float eps, int32_t bits, int16_t* h, int8_t* y, float* scales,
+                            void* stream);
+
+/*
+ * A paged cache of keys and values.  Its arrays and sizes, for the three calls below:
+ *
+ *   k_pages  [pages, Hkv, page, d] int8, 16-byte aligned: a row for each key.
+ *   v_pages  [pages, Hkv, d, page] int8, 16-byte aligned: a row for each channel.
+ *   weight   [pages, Hkv, page] int64, 8-byte aligned: the attention weight that each
+ *            key has received (NULL where it is not collected).
+ *   table    [B, max_pages] int32: sequence b's key at place p lies in slot p % page of
+ *            page table[b, p / page].  Entries behind a sequence's last key are not read.
+ *   length   [B] int32: keys of each sequence, in [0, max_pages page].
+ * pages in [1, 2^30], page a power of two in [16, 1024], d a multiple of 16 in
+ * [16, 128], max_pages page at most 2^20, Hkv in [1, 1024], B Hkv in [0, 65536].
+ * table and length are device arrays and cannot be checked here: a length is taken
+ * within [0, max_pages page]; a table entry that names no page reads as page 0 and is
+ * never written through.  Sequences may share pages that no call writes.
+ */
+
+/*
+ * Writes the keys and values of new tokens (as rope_qkv_int8 gives them) into a cache,
+ * and a weight of 0.
+ *
+ *   k, v    [B, Hkv, L, d] int8, 16-byte aligned, L in [0, 2^20].
+ *   n_new   NULL (L for every sequence) or [B] int32 in [0, L]: token i < n_new[b] of
+ *           sequence b goes to place length[b] - n_new[b] + i, so length counts the new
+ *           tokens.  Rows behind n_new[b] are not read; a token whose place is negative
+ *           or beyond the table is left out.
+ * All other slots are left as they were.  Places of two tokens that are one slot (pages
+ * in the table twice) hold either token's bytes.
+ * Errors: FQ_ERR_NULL (all but weight and n_new), FQ_ERR_SHAPE (sizes, or 2^24 or more
+ * workgroups: B Hkv (L / 64 + 2)), FQ_ERR_PARAM (alignment).
+ */
+fq_status kv_cache_append_int8(const int8_t* k, const int8_t* v, int32_t B, int32_t Hkv, int32_t L,
+                               int32_t d, const int32_t* n_new, int8_t* k_pages, int8_t* v_pages,
+                               int64_t* weight, int32_t pages, int32_t page, const int32_t* table,
+                               int32_t max_pages, const int32_t* length, void* stream);
+
+/*
+ * Attention of new tokens over a cache: lis_attention_qk's operator (MinMax-quantized
+ * MatMul, Log-Int-Softmax, BitShift product) for rows of any length, of which each sees
+ * a part, with shared key heads.
+ *
+ *   q       [B, Hq, L, d] int8 container, 16-byte aligned, zp_q; Hq = r Hkv, and head
+ *           hq reads key head hq / r.  L in [0, 2^20], L r below 2^30.
+ *   n_new   NULL (L) or [B] int32 in [0, L]: token i < n_new[b] stands at place
+ *           length[b] - n_new[b] + i.  Rows behind n_new[b] are neither read nor written.
+ *   causal  1: a token sees the places up to its own; 0: all keys of its sequence.
+ *   zp_k    does not change the result (see lis_attention_qk); it is validated.
+ *   s_logit, bits (in [1, 4]), exp_n: as in lis_attention_head.
+ *   out     [B, Hq, L, d] int32, 16-byte aligned: for a token that sees the keys J,
+ *           out[c] = sum_{j in J} (v[j, c] - zp_v) 2^(2^b - 1 - code_j)
+ *           with the codes of Log-Int-Softmax over J; 0 where J is empty.
+ *   weight  NULL, or the cache's: weight[key's slot] += sum over the tokens and the r heads
+ *           of its key head of 2^(2^b - 1 - code), 0 for a token that does not see it.
+ *           (64-bit integer atomics: the sums do not depend on their order.)
+ *   workspace  device scratch of fq_lis_attention_paged_workspace_bytes(B, Hq, Hkv, L,
+ *           d, max_pages * page) bytes, 16-byte aligned, of one call at a time (NULL where that
+ *           is 0); its contents on entry do not matter.
+ * Every row's sum is exact in 64 bits and out in 32: |out| <= 255 (1.5 2^15 + 2^20).
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (sizes, Hq, or 2^24 or more workgroups), FQ_ERR_PARAM
+ * (zero points, causal, bits, exp_n, s_logit, alignment, workspace too small),
+ * FQ_ERR_HEADROOM (that of lis_softmax_log4 with Lk = max_pages page).
+ */
+size_t fq_lis_attention_paged_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t L,
+                                              int32_t d, int64_t max_keys);
+fq_status lis_attention_paged(const int8_t* q, int32_t B, int32_t Hq, int32_t Hkv, int32_t L,
+                              int32_t d, const int32_t* n_new, const int8_t* k_pages,
+                              const int8_t* v_pages, int64_t* weight, int32_t pages, int32_t page,
+                              const int32_t* table, int32_t max_pages, const int32_t* length,
+                              int32_t zp_q, int32_t zp_k, int32_t zp_v, int32_t causal,
+                              float s_logit, int32_t bits, int32_t exp_n, int32_t* out,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Cuts each sequence of a cache to at most `keep` keys, by each key head on its own: the
+ * `recent` last keys stay and, of the others, those of the largest weight (of equal ones
+ * the first), keep in all.  They keep their order and are brought together in the
+ * places [0, keep) of the pages that table_out names.
+ *
+ *   keep    in [1, 2^20]; recent in [0, keep].
+ *   table_out  [B, max_out] int32, max_out page >= keep: table itself (in place, with
+ *           max_out = max_pages) or pages that no other sequence's entries of
+ *           either table name.  In place, a sequence's pages are its own.
+ *   length_out [B] int32 (out): min(length, keep); it may be length itself.
+ *   kept    [B, Hkv, keep] int32 (out): the places that stayed, ascending; -1 behind the last.
+ *           A sequence of at most `keep` keys keeps them all (in other pages: is copied).
+ * Slots behind the last key that stayed are left as they were.  The cache's weight may
+ * not be NULL.
+ * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (sizes, keep, max_out), FQ_ERR_PARAM (recent, alignment).
+ */
+fq_status kv_cache_evict(int8_t* k_pages, int8_t* v_pages, int64_t* weight, int32_t pages,
+                         int32_t Hkv, int32_t page, int32_t d, const int32_t* table,
+                         int32_t max_pages, const int32_t* length, int32_t B, int32_t keep,
+                         int32_t recent, const int32_t* table_out, int32_t max_out,
+                         int32_t* length_out, int32_t* kept, void* stream);
 
 #ifdef __cplusplus
 }

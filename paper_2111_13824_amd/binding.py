@@ -48,6 +48,20 @@ SIGNATURES = {
     "requant_heads_int8": [_P, _I64, _I32, _I32, _I32, _F32, _F32, _I32, _I32, _P, _P],
     "fq_activation_table": [_I32, _F32, _I32, _I32, _F32, _P],
 }
+# The entry points of a step over a stream of tokens (decode.py).
+DECODE_SIGNATURES = {
+    "rmsnorm_int8": [_P, _I32, _P, _I32, _F32, _P, _I64, _I32, _P, _F32, _F32, _I32, _I32, _P, _P,
+                     _P],
+    "rmsnorm_rows_int8": [_P, _I32, _P, _I32, _F32, _P, _I64, _I32, _P, _F32, _I32, _P, _P, _P, _P],
+    "kv_cache_append_int8": [_P, _P, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _I32, _I32, _P, _I32,
+                             _P, _P],
+    "lis_attention_paged": [_P, _I32, _I32, _I32, _I32, _I32, _P, _P, _P, _P, _I32, _I32, _P, _I32,
+                            _P, _I32, _I32, _I32, _I32, _F32, _I32, _I32, _P, _P, ctypes.c_size_t,
+                            _P],
+    "kv_cache_evict": [_P, _P, _P, _I32, _I32, _I32, _I32, _P, _I32, _P, _I32, _I32, _I32, _P, _I32,
+                       _P, _P, _P],
+}
+_TYPES = {**SIGNATURES, **DECODE_SIGNATURES}
 
 
 def _int32s(types):
@@ -57,7 +71,7 @@ def _int32s(types):
     return operator.itemgetter(*at), struct.Struct(f"={len(at)}i").pack
 
 
-_INT32S = {name: _int32s(types) for name, types in SIGNATURES.items()}
+_INT32S = {name: _int32s(types) for name, types in _TYPES.items()}
 
 # Activations of linear_int8 and functions of fq_activation_table.
 ACT_NONE, ACT_RELU, ACT_TABLE = range(3)
@@ -76,7 +90,7 @@ _lib: Optional[ctypes.CDLL] = None
 def load(path: str) -> ctypes.CDLL:
     """Open a build of libfqvit at `path` and declare its entry points' C types."""
     L = ctypes.CDLL(path)
-    for name, args in SIGNATURES.items():
+    for name, args in _TYPES.items():
         fn = getattr(L, name)
         fn.argtypes = args
         fn.restype = ctypes.c_int32
@@ -88,6 +102,8 @@ def load(path: str) -> ctypes.CDLL:
     L.fq_time_next_call.restype = ctypes.c_int32
     L.fq_ptf_calibrate_workspace_bytes.argtypes = [_I64, _I32, _I32]
     L.fq_ptf_calibrate_workspace_bytes.restype = ctypes.c_size_t
+    L.fq_lis_attention_paged_workspace_bytes.argtypes = [_I32] * 5 + [_I64]
+    L.fq_lis_attention_paged_workspace_bytes.restype = ctypes.c_size_t
     return L
 
 
@@ -177,7 +193,7 @@ class Prepared:
         self._name = name
         self._fn = getattr(lib(), name)
         self._args = tuple(t(a) if a is not None else None
-                           for t, a in zip(SIGNATURES[name], args))
+                           for t, a in zip(_TYPES[name], args))
         self._keep = keep
         self._device = device
 

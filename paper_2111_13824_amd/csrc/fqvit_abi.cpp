@@ -9,6 +9,7 @@
 
 #include "fqvit_internal.h"
 #include "layers_internal.h"
+#include "stream_internal.h"
 
 namespace {
 
@@ -540,6 +541,185 @@ fq_status requant_heads_int8(const int32_t* q, int64_t B, int32_t H, int32_t L, 
     a.L = L;
     a.d = d;
     return launched(fqvit::launch_requant_heads, a, stream);
+}
+
+namespace {
+
+fq_status rmsnorm(const int8_t* x, int32_t zp_x, const uint8_t* alpha, int32_t K, float m_x,
+                  const int16_t* r, int64_t T, int32_t C, const float* gamma, float eps, float s_out,
+                  int32_t zp_out, int32_t bits, int16_t* h, int8_t* y, float* scales, bool rows,
+                  void* stream) {
+    ConsumeEvents consume;
+    if (T < 0 || T >= ((int64_t)1 << 24) || C < 1 || C > kMaxC) return FQ_ERR_SHAPE;
+    if (bits < 2 || bits > 8 || !(eps >= 0.0f) || !std::isfinite(eps)) return FQ_ERR_PARAM;
+    const int32_t half = 1 << (bits - 1);
+    if (!rows && (!positive(s_out) || zp_out < -half || zp_out >= half)) return FQ_ERR_PARAM;
+    // (x - zp_x) 2^K m_x stays below 2^21
+    if (x && (!int8_zp(zp_x) || !(m_x >= 0x1p-20f && m_x <= 64.0f))) return FQ_ERR_PARAM;
+    if (x && alpha && (K < 0 || K > 7)) return FQ_ERR_PARAM;
+    if (T == 0) return FQ_OK;
+    if (!r || !gamma || !h || !y || (rows && !scales)) return FQ_ERR_NULL;
+    fqvit::RmsArgs a{};
+    a.x = x;
+    a.alpha = x ? alpha : nullptr;
+    a.zp_x = zp_x;
+    a.K = K;
+    a.m_x = m_x;
+    a.r = r;
+    a.gamma = gamma;
+    a.T = T;
+    a.C = C;
+    a.eps = eps;
+    a.s_out = s_out;
+    a.zp_out = zp_out;
+    a.bits = bits;
+    a.h = h;
+    a.y = y;
+    a.scales = scales;
+    return launched(fqvit::launch_rmsnorm, a, stream);
+}
+
+constexpr int32_t kMaxCacheD = 128;
+constexpr int32_t kMaxPage = 1024;
+constexpr int64_t kMaxCacheKeys = (int64_t)1 << 20;
+constexpr int64_t kMaxUnits = 65536;                    // sequences times key heads
+constexpr int64_t kMaxGroups = (int64_t)1 << 24;        // workgroups of 256: fewer than 2^32 threads
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Sizes of a cache; its view.
+bool cache_view(int8_t* k, int8_t* v, int64_t* weight, const int32_t* table, const int32_t* length,
+                int32_t pages, int32_t page, int32_t max_pages, int32_t B, int32_t Hkv, int32_t d,
+                fqvit::CacheView* c) {
+    if (pages < 1 || pages > (1 << 30) || page < 16 || page > kMaxPage || (page & (page - 1)) != 0 ||
+        max_pages < 1 || (int64_t)max_pages * page > kMaxCacheKeys || B < 0 || Hkv < 1 ||
+        Hkv > kMaxHeads || (int64_t)B * Hkv > kMaxUnits || d < 16 || d > kMaxCacheD || d % 16 != 0)
+        return false;
+    int32_t log2_page = 0;
+    while ((1 << log2_page) < page) ++log2_page;
+    *c = fqvit::CacheView{k, v, weight, table, length, pages, max_pages, log2_page, B, Hkv, d};
+    return true;
+}
+
+}  // namespace
+
+fq_status rmsnorm_int8(const int8_t* x, int32_t zp_x, const uint8_t* alpha, int32_t K, float m_x,
+                       const int16_t* r, int64_t T, int32_t C, const float* gamma, float eps,
+                       float s_out, int32_t zp_out, int32_t bits, int16_t* h, int8_t* y,
+                       void* stream) {
+    return rmsnorm(x, zp_x, alpha, K, m_x, r, T, C, gamma, eps, s_out, zp_out, bits, h, y, nullptr,
+                   false, stream);
+}
+
+fq_status rmsnorm_rows_int8(const int8_t* x, int32_t zp_x, const uint8_t* alpha, int32_t K,
+                            float m_x, const int16_t* r, int64_t T, int32_t C, const float* gamma,
+                            float eps, int32_t bits, int16_t* h, int8_t* y, float* scales,
+                            void* stream) {
+    return rmsnorm(x, zp_x, alpha, K, m_x, r, T, C, gamma, eps, 1.0f, 0, bits, h, y, scales, true,
+                   stream);
+}
+
+fq_status kv_cache_append_int8(const int8_t* k, const int8_t* v, int32_t B, int32_t Hkv, int32_t L,
+                               int32_t d, const int32_t* n_new, int8_t* k_pages, int8_t* v_pages,
+                               int64_t* weight, int32_t pages, int32_t page, const int32_t* table,
+                               int32_t max_pages, const int32_t* length, void* stream) {
+    ConsumeEvents consume;
+    fqvit::AppendArgs a{};
+    if (!cache_view(k_pages, v_pages, weight, table, length, pages, page, max_pages, B, Hkv, d, &a.c) ||
+        L < 0 || L > kMaxCacheKeys || (int64_t)B * Hkv * (L / 64 + 2) >= kMaxGroups)
+        return FQ_ERR_SHAPE;
+    if (B == 0 || L == 0) return FQ_OK;
+    if (!k || !v || !k_pages || !v_pages || !table || !length) return FQ_ERR_NULL;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) ||
+        !aligned(weight, 8))
+        return FQ_ERR_PARAM;
+    a.k = k;
+    a.v = v;
+    a.n_new = n_new;
+    a.L = L;
+    return launched(fqvit::launch_kv_append, a, stream);
+}
+
+namespace {
+
+// Sizes of queries over a cache whose view holds.
+bool query_sizes(int32_t B, int32_t Hq, int32_t Hkv, int32_t L) {
+    if (Hq < 1 || Hq > kMaxHeads || Hkv < 1 || Hq % Hkv != 0 || L < 0 || L > kMaxCacheKeys) return false;
+    const int64_t rows = (int64_t)L * (Hq / Hkv);
+    return rows < ((int64_t)1 << 30) && (int64_t)B * Hkv * (rows / 16 + 1) < kMaxGroups;
+}
+
+}  // namespace
+
+size_t fq_lis_attention_paged_workspace_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t L,
+                                              int32_t d, int64_t max_keys) {
+    if (B < 1 || Hkv < 1 || !query_sizes(B, Hq, Hkv, L) || L < 1 || d < 1 || max_keys < 1 ||
+        max_keys > kMaxCacheKeys)
+        return 0;
+    return fqvit::lis_paged_workspace ? fqvit::lis_paged_workspace(B, Hq, Hkv, L, d, max_keys) : 0;
+}
+
+fq_status lis_attention_paged(const int8_t* q, int32_t B, int32_t Hq, int32_t Hkv, int32_t L,
+                              int32_t d, const int32_t* n_new, const int8_t* k_pages,
+                              const int8_t* v_pages, int64_t* weight, int32_t pages, int32_t page,
+                              const int32_t* table, int32_t max_pages, const int32_t* length,
+                              int32_t zp_q, int32_t zp_k, int32_t zp_v, int32_t causal,
+                              float s_logit, int32_t bits, int32_t exp_n, int32_t* out,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    ConsumeEvents consume;
+    fqvit::PagedArgs a{};
+    if (!cache_view(const_cast<int8_t*>(k_pages), const_cast<int8_t*>(v_pages), weight, table, length,
+                    pages, page, max_pages, B, Hkv, d, &a.c) ||
+        !query_sizes(B, Hq, Hkv, L))
+        return FQ_ERR_SHAPE;
+    if (!int8_zp(zp_q) || !int8_zp(zp_k) || !int8_zp(zp_v) || bits > 4 || (causal != 0 && causal != 1))
+        return FQ_ERR_PARAM;
+    const fq_status st = lis_constants(s_logit, bits, exp_n, max_pages * page, &a.k);
+    if (st != FQ_OK) return st;
+    if (B == 0 || L == 0) return FQ_OK;
+    if (!q || !k_pages || !v_pages || !table || !length || !out) return FQ_ERR_NULL;
+    const size_t need =
+        fq_lis_attention_paged_workspace_bytes(B, Hq, Hkv, L, d, (int64_t)max_pages * page);
+    if (need && !workspace) return FQ_ERR_NULL;
+    if (workspace_bytes < need || !aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) ||
+        !aligned(out, 16) || !aligned(weight, 8) || (need && !aligned(workspace, 16)))
+        return FQ_ERR_PARAM;
+    a.q = q;
+    a.n_new = n_new;
+    a.Hq = Hq;
+    a.L = L;
+    a.group = Hq / Hkv;
+    a.zp_q = zp_q;
+    a.zp_v = zp_v;
+    a.causal = causal;
+    a.out = out;
+    a.workspace = workspace;
+    return launched(fqvit::launch_lis_paged, a, stream);
+}
+
+fq_status kv_cache_evict(int8_t* k_pages, int8_t* v_pages, int64_t* weight, int32_t pages,
+                         int32_t Hkv, int32_t page, int32_t d, const int32_t* table,
+                         int32_t max_pages, const int32_t* length, int32_t B, int32_t keep,
+                         int32_t recent, const int32_t* table_out, int32_t max_out,
+                         int32_t* length_out, int32_t* kept, void* stream) {
+    ConsumeEvents consume;
+    fqvit::EvictArgs a{};
+    if (!cache_view(k_pages, v_pages, weight, table, length, pages, page, max_pages, B, Hkv, d, &a.c) ||
+        keep < 1 || keep > kMaxCacheKeys || max_out < 1 || (int64_t)max_out * page > kMaxCacheKeys ||
+        (int64_t)max_out * page < keep || (table_out == table && max_out != max_pages))
+        return FQ_ERR_SHAPE;
+    if (recent < 0 || recent > keep) return FQ_ERR_PARAM;
+    if (B == 0) return FQ_OK;
+    if (!k_pages || !v_pages || !weight || !table || !length || !table_out || !length_out || !kept)
+        return FQ_ERR_NULL;
+    if (!aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(weight, 8)) return FQ_ERR_PARAM;
+    a.table_out = table_out;
+    a.max_out = max_out;
+    a.keep = keep;
+    a.recent = recent;
+    a.length_out = length_out;
+    a.kept = kept;
+    return launched(fqvit::launch_kv_evict, a, stream);
 }
 
 }  // extern "C"
