@@ -1,0 +1,58 @@
+// How a call of the attention over a paged cache is divided: chosen on the host from
+// its sizes alone (lengths are device data).
+#pragma once
+
+#include <stdint.h>
+
+#include "stream_internal.h"
+
+namespace fqvit {
+namespace paged {
+
+constexpr int kWaves = 4;           // wavefronts of a workgroup
+constexpr int kTile = 64;           // keys a wavefront takes at a time
+
+struct Plan {
+    int32_t stored;         // logits kept in the workspace between the passes (at most 16 rows)
+    int32_t splits;         // parts of the keys, each a workgroup's; more than one: three launches
+    int32_t sets;           // sets of 16 rows a wavefront holds
+    int32_t row_groups;     // row groups of a workgroup; the other wavefronts share its keys
+    int32_t tiles;          // workgroups over the rows of a sequence and key head
+    int32_t rows;           // rows of a sequence and key head
+    int64_t units;          // sequences times key heads
+    int64_t keys;           // keys a table names, up to a multiple of 64
+
+    int64_t tile_rows() const { return (int64_t)16 * sets * row_groups; }
+    // workspace: maxima [units, tiles, splits, tile_rows] int32, sums of 64 bits
+    // likewise, then the logits [units, rows, keys] int32
+    size_t partials() const { return splits > 1 ? (size_t)(units * tiles * splits * tile_rows()) : 0; }
+    size_t logits() const { return stored ? (size_t)(units * rows * keys) : 0; }
+    size_t bytes() const { return partials() * 12 + logits() * 4; }
+};
+
+inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int64_t max_keys) {
+    Plan p{};
+    p.units = (int64_t)B * Hkv;
+    p.rows = L * (Hq / Hkv);
+    p.keys = (max_keys + kTile - 1) / kTile * kTile;
+    p.splits = 1;
+    p.sets = p.rows > 16 ? 2 : 1;
+    p.row_groups = 1;
+    if (p.rows > 64) p.row_groups = 2;
+    const auto count = [&] { return (int32_t)((p.rows + p.tile_rows() - 1) / p.tile_rows()); };
+    p.tiles = count();
+    const int64_t groups = p.units * p.tiles;
+    // parts of at least 512 keys until there are four workgroups a compute unit
+    const int64_t most = p.keys / 512;
+    int64_t want = 1024 / (groups > 0 ? groups : 1);
+    if (want > most) want = most;
+    if (want > 256) want = 256;
+    if (p.keys > 1024 && want > 1) {
+        p.splits = (int32_t)want;
+        p.stored = p.rows <= 16;
+    }
+    return p;
+}
+
+}  // namespace paged
+}  // namespace fqvit
