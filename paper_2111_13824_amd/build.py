@@ -21,7 +21,9 @@ SOURCES = ["ptf_layernorm.hip", "lis_attention.hip", "lis_inst_lo.hip", "lis_ins
            "linear_tile.hip:FQ_TILE_W=3", "linear_tile.hip:FQ_TILE_W=4",
            "linear_tile.hip:FQ_TILE_W=5", "linear_tile.hip:FQ_TILE_128",
            "linear_tile.hip:FQ_TILE_64", "linear_tile.hip:FQ_TILE_256R", "heads.hip",
-           "rmsnorm.hip", "kv_cache.hip", "lis_paged.hip", "fqvit_abi.cpp"]     # "file:MACRO": compiled with -DMACRO
+           "rmsnorm.hip", "kv_cache.hip", "lis_paged.hip",
+           "lis_paged.hip:FQ_PAGED_32", "lis_paged.hip:FQ_PAGED_64", "lis_paged.hip:FQ_PAGED_128",
+           "fqvit_abi.cpp"]     # "file:MACRO": compiled with -DMACRO
 OBJDIR = os.path.join(HERE, "_build")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -44,6 +44,7 @@ using cache::page_at;
 using paged::kTile;
 using paged::kWaves;
 using paged::Plan;
+using paged::Shape;
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
@@ -51,15 +52,6 @@ constexpr int kBlock = 64 * kWaves;
 
 // Passes of a launch: all of them, or one where the keys are divided.
 enum Pass { kAll, kMax, kSum, kOut };
-
-struct Shape {
-    int32_t splits, row_groups, tiles, rows;
-    int64_t keys;               // row stride of the stored logits
-    int32_t* part_max;          // [units, tiles, splits, rows of a tile]
-    uint64_t* part_sum;
-    int32_t* logits;            // [units, rows, keys]
-    int32_t shift, buckets;     // of the thresholds' buckets
-};
 
 // Row rho of a sequence and head is query (token rho / group, head rho % group).
 __device__ __forceinline__ int64_t query_of(const PagedArgs& a, int b, int h, int rho) {
@@ -237,22 +229,30 @@ template <bool FAST>
 struct RowAdder {
     uint64_t sum = 0;
 
+    // P0: the I-Exp needs no pre-shift (q_ln2 above 512)
+    template <bool P0>
+    __device__ __forceinline__ void fast(const i32x4 (&acc)[4], const PagedArgs& a, bool edge, int key0,
+                                         int limit, int lane) {
+        const double unit = __longlong_as_double((int64_t)(1023 + 52 - a.k.n) << 52);
+        double s0 = unit, s1 = unit;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t e = lis::screen_iexp<P0>(acc[t][i], 0, a.k);       // the row's offset is in acc
+                if (edge) e = seen(key0, t, i, limit, lane) ? e : 0u;
+                if (i & 1) s1 += (double)__uint_as_float(e);
+                else s0 += (double)__uint_as_float(e);
+            }
+        const uint64_t m = (1ull << 52) - 1;
+        sum += ((uint64_t)__double_as_longlong(s0) & m) + ((uint64_t)__double_as_longlong(s1) & m);
+    }
+
     __device__ __forceinline__ void add(const i32x4 (&acc)[4], int mx, const PagedArgs& a, bool edge,
                                         int key0, int limit, int lane) {
         if constexpr (FAST) {
-            const double unit = __longlong_as_double((int64_t)(1023 + 52 - a.k.n) << 52);
-            double s0 = unit, s1 = unit;
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t e = lis::screen_iexp(acc[t][i], 0, a.k);       // the row's offset is in acc
-                    if (edge) e = seen(key0, t, i, limit, lane) ? e : 0u;
-                    if (i & 1) s1 += (double)__uint_as_float(e);
-                    else s0 += (double)__uint_as_float(e);
-                }
-            const uint64_t m = (1ull << 52) - 1;
-            sum += ((uint64_t)__double_as_longlong(s0) & m) + ((uint64_t)__double_as_longlong(s1) & m);
+            if (a.k.s_pre == 0) fast<true>(acc, a, edge, key0, limit, lane);
+            else fast<false>(acc, a, edge, key0, limit, lane);
         } else {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -279,24 +279,25 @@ __device__ __forceinline__ void digits(uint32_t m, uint32_t& hi, uint32_t& lo) {
     lo = v & ~up;
 }
 
-template <int RS, int KS, int NV, Pass PASS, bool STORED, bool FAST>
-__global__ __launch_bounds__(kBlock) void lis_paged_kernel(PagedArgs a, Shape sh) {
+template <int RS, int KS, int NV, Pass PASS, bool STORED, bool FAST, bool WEIGHT>
+__global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape sh) {
     constexpr int kRows = 16 * RS;
     extern __shared__ uint32_t dyn[];               // buckets, then the workgroup's out
     __shared__ int row_max[kRows * kWaves];
     __shared__ unsigned long long row_sum[kRows * kWaves];
     __shared__ int U[kRows * kWaves][kMaxTop];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int RG = sh.row_groups, KG = kWaves / RG;
     const int rg = wave / KG, kg = wave - rg * KG;
     const int tile_rows = RG * kRows;
-    const int64_t block = lis::xcd_remap(blockIdx.x, gridDim.x);
-    const int split = (int)(block % sh.splits);
-    const int64_t wg = block / sh.splits;
-    const int tile = sh.tiles - 1 - (int)(wg % sh.tiles);       // the rows that see most come first
-    const int64_t unit = wg / sh.tiles;
-    const int b = (int)(unit / a.c.Hkv), h = (int)(unit % a.c.Hkv);
+    // fewer than 2^24 workgroups: 32-bit divisions
+    const uint32_t block = (uint32_t)lis::xcd_remap(blockIdx.x, gridDim.x);
+    const uint32_t wg = block / (uint32_t)sh.splits;
+    const int split = (int)(block - wg * (uint32_t)sh.splits);
+    const int64_t unit = wg / (uint32_t)sh.tiles;
+    const int tile = sh.tiles - 1 - (int)(wg - (uint32_t)unit * (uint32_t)sh.tiles);    // the rows that see most come first
+    const int b = (int)((uint32_t)unit / (uint32_t)a.c.Hkv), h = (int)unit - b * a.c.Hkv;
     const int len = keys_of(a.c, b);
     const int fresh = a.n_new ? min(max(a.n_new[b], 0), a.L) : a.L;
     const int rows = fresh * a.group;
@@ -472,7 +473,8 @@ __global__ __launch_bounds__(kBlock) void lis_paged_kernel(PagedArgs a, Shape sh
                 for (int i = 0; i < 4; ++i) {
                     if (FAST) {
                         // -u; a key that the row does not see may lie above its maximum
-                        const int u = min(max(acc[s][t][i], -cap), 0);
+                        int u;
+                        asm("v_med3_i32 %0, %1, %2, 0" : "=v"(u) : "v"(acc[s][t][i]), "s"(-cap));
                         x[i] = end[(u >> sh.shift) * 16] + (uint32_t)u;
                     } else {
                         uint32_t z;
@@ -507,7 +509,7 @@ __global__ __launch_bounds__(kBlock) void lis_paged_kernel(PagedArgs a, Shape sh
                 ph[s] = mfma(ones, wh, ph[s]);
                 pl[s] = mfma(ones, wl, pl[s]);
             }
-            if (a.c.weight) {
+            if (WEIGHT) {
                 const bool mine = row0 + 16 * s + (lane & 15) < rows;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -583,11 +585,11 @@ template <bool FAST>
 __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shape sh) {
     __shared__ int row_max[16];
     __shared__ unsigned long long row_sum[16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t block = lis::xcd_remap(blockIdx.x, gridDim.x);
-    const int split = (int)(block % sh.splits);
-    const int64_t unit = block / sh.splits;
-    const int b = (int)(unit / a.c.Hkv);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t block = (uint32_t)lis::xcd_remap(blockIdx.x, gridDim.x);
+    const int64_t unit = block / (uint32_t)sh.splits;
+    const int split = (int)(block - (uint32_t)unit * (uint32_t)sh.splits);
+    const int b = (int)((uint32_t)unit / (uint32_t)a.c.Hkv);
     const int len = keys_of(a.c, b);
     const int fresh = a.n_new ? min(max(a.n_new[b], 0), a.L) : a.L;
     const int rows = fresh * a.group;
@@ -654,41 +656,58 @@ void enqueue(const PagedArgs& a, const Shape& sh, const Plan& p, bool fast, hipS
     const bool shared_out = last && (p.row_groups < kWaves || PASS == kOut);
     const size_t lds = 4 * ((last && fast ? (size_t)p.tile_rows() * sh.buckets : 0) +
                             (shared_out ? (size_t)p.tile_rows() * a.c.d : 0));
-    launch_kernel(fast ? lis_paged_kernel<RS, KS, NV, PASS, STORED, true>
-                       : lis_paged_kernel<RS, KS, NV, PASS, STORED, false>,
+    constexpr bool kWeight = PASS == kAll || PASS == kOut;
+    const bool weight = kWeight && a.c.weight;
+    launch_kernel(fast ? (weight ? lis_paged_kernel<RS, KS, NV, PASS, STORED, true, kWeight>
+                                 : lis_paged_kernel<RS, KS, NV, PASS, STORED, true, false>)
+                       : (weight ? lis_paged_kernel<RS, KS, NV, PASS, STORED, false, kWeight>
+                                 : lis_paged_kernel<RS, KS, NV, PASS, STORED, false, false>),
                   dim3((uint32_t)(p.units * p.tiles * p.splits)), dim3(kBlock), lds, stream, a, sh);
 }
 
-template <int KS, int NV>
+// RS: sets of rows a wavefront holds where there are more than 16 rows
+template <int RS, int KS, int NV>
 void launch(const PagedArgs& a, const Shape& sh, const Plan& p, hipStream_t stream) {
     const bool fast = fast_path(a.k);
     if (p.splits == 1) {
         if (p.sets == 1) enqueue<1, KS, NV, kAll, false>(a, sh, p, fast, stream);
-        else enqueue<2, KS, NV, kAll, false>(a, sh, p, fast, stream);
+        else enqueue<RS, KS, NV, kAll, false>(a, sh, p, fast, stream);
         return;
     }
     const LaunchEvents ev = launch_events();
     set_launch_events(ev.start, nullptr);
     if (p.stored) enqueue<1, KS, NV, kMax, true>(a, sh, p, fast, stream);
-    else enqueue<2, KS, NV, kMax, false>(a, sh, p, fast, stream);
+    else enqueue<RS, KS, NV, kMax, false>(a, sh, p, fast, stream);
     set_launch_events(nullptr, nullptr);
     if (p.stored)
         launch_kernel(fast ? lis_paged_sum_kernel<true> : lis_paged_sum_kernel<false>,
                       dim3((uint32_t)(p.units * p.splits)), dim3(kBlock), 0, stream, a, sh);
-    else enqueue<2, KS, NV, kSum, false>(a, sh, p, fast, stream);
+    else enqueue<RS, KS, NV, kSum, false>(a, sh, p, fast, stream);
     set_launch_events(nullptr, ev.stop);
     if (p.stored) enqueue<1, KS, NV, kOut, true>(a, sh, p, fast, stream);
-    else enqueue<2, KS, NV, kOut, false>(a, sh, p, fast, stream);
+    else enqueue<RS, KS, NV, kOut, false>(a, sh, p, fast, stream);
 }
 
 }  // namespace
 
-size_t lis_paged_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_t, int64_t max_keys) {
-    return paged::plan(B, Hq, Hkv, L, max_keys).bytes();
+#if defined(FQ_PAGED_32)
+void launch_lis_paged_32(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<2, 1, 2>(a, sh, p, s); }
+#elif defined(FQ_PAGED_64)
+void launch_lis_paged_64(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<2, 1, 4>(a, sh, p, s); }
+#elif defined(FQ_PAGED_128)
+void launch_lis_paged_128(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<1, 2, 8>(a, sh, p, s); }
+#else
+void launch_lis_paged_32(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s);
+void launch_lis_paged_64(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s);
+void launch_lis_paged_128(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s);
+
+size_t lis_paged_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_t d,
+                           int64_t max_keys) {
+    return paged::plan(B, Hq, Hkv, L, d, max_keys).bytes();
 }
 
 hipError_t launch_lis_paged(const PagedArgs& a, hipStream_t stream) {
-    const Plan p = paged::plan(a.c.B, a.Hq, a.c.Hkv, a.L, (int64_t)a.c.max_pages << a.c.log2_page);
+    const Plan p = paged::plan(a.c.B, a.Hq, a.c.Hkv, a.L, a.c.d, (int64_t)a.c.max_pages << a.c.log2_page);
     Shape sh{};
     sh.splits = p.splits;
     sh.row_groups = p.row_groups;
@@ -702,10 +721,11 @@ hipError_t launch_lis_paged(const PagedArgs& a, hipStream_t stream) {
     while ((2u << sh.shift) * 2 <= a.k.d_ln2) ++sh.shift;       // 2^shift <= q_ln2 / 2
     const int cap = (a.k.n < a.k.top ? a.k.n : a.k.top) * (int)a.k.d_ln2;
     sh.buckets = ((cap - 1) >> sh.shift) + 2;
-    if (a.c.d <= 32) launch<1, 2>(a, sh, p, stream);
-    else if (a.c.d <= 64) launch<1, 4>(a, sh, p, stream);
-    else launch<2, 8>(a, sh, p, stream);
+    if (a.c.d <= 32) launch_lis_paged_32(a, sh, p, stream);
+    else if (a.c.d <= 64) launch_lis_paged_64(a, sh, p, stream);
+    else launch_lis_paged_128(a, sh, p, stream);
     return hipGetLastError();
 }
+#endif
 
 }  // namespace fqvit

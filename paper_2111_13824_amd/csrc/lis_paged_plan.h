@@ -30,13 +30,24 @@ struct Plan {
     size_t bytes() const { return partials() * 12 + logits() * 4; }
 };
 
-inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int64_t max_keys) {
+// What a kernel is told of it.
+struct Shape {
+    int32_t splits, row_groups, tiles, rows;
+    int64_t keys;               // row stride of the stored logits
+    int32_t* part_max;          // [units, tiles, splits, rows of a tile]
+    uint64_t* part_sum;
+    int32_t* logits;            // [units, rows, keys]
+    int32_t shift, buckets;     // of the thresholds' buckets
+};
+
+inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_t d, int64_t max_keys) {
     Plan p{};
     p.units = (int64_t)B * Hkv;
     p.rows = L * (Hq / Hkv);
     p.keys = (max_keys + kTile - 1) / kTile * kTile;
     p.splits = 1;
-    p.sets = p.rows > 16 ? 2 : 1;
+    // two sets of rows share the operands of the keys; wide heads' results leave room for one
+    p.sets = p.rows > 16 && d <= 64 ? 2 : 1;
     p.row_groups = 1;
     if (p.rows > 64) p.row_groups = 2;
     const auto count = [&] { return (int32_t)((p.rows + p.tile_rows() - 1) / p.tile_rows()); };
