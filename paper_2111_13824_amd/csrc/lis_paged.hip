@@ -9,7 +9,12 @@
 // r: a row's maximum, sum and thresholds belong to one register of its lane, its codes
 // need no exchange, and the 16 weights P of a lane are, as bytes, its operand of the
 // second product D = V^T P^T.  The V^T operand is 16 neighbouring keys of a channel:
-// the cache holds values with their channels in rows.  No operand goes through LDS.
+// the cache holds values with their channels in rows.
+//
+// Tiles of keys and values come into LDS in the order of memory, a stage of a few tiles at
+// a time, loaded three stages ahead; a workgroup's wavefronts share them.  (Loaded straight into the operands' registers,
+// 16 neighbouring lanes read 16 rows: the chunks of 8 x 16 heads x 512 tokens over 4096
+// keys took 214 us, of which the vector instructions were a third.)
 //
 // A weight P = 2^m, m = (2^b - 1) - code in [0, 15], is not an int8: it is taken as
 // -256 hi - lo with hi, lo in {0, -1, -2, .. -128}, two products with the same V
@@ -42,16 +47,18 @@ using cache::head_base;
 using cache::keys_of;
 using cache::page_at;
 using paged::kTile;
-using paged::kWaves;
 using paged::Plan;
 using paged::Shape;
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kBlock = 64 * kWaves;
+constexpr int kBlock = 256;         // of the sums over stored logits
 
 // Passes of a launch: all of them, or one where the keys are divided.
 enum Pass { kAll, kMax, kSum, kOut };
+// Arithmetic: 64-bit steps of any constants; thresholds and the binary32 I-Exp; the same
+// without its pre-shift (q_ln2 above 512).
+enum Mode { kGeneral, kShifted, kPlain };
 
 // Row rho of a sequence and head is query (token rho / group, head rho % group).
 __device__ __forceinline__ int64_t query_of(const PagedArgs& a, int b, int h, int rho) {
@@ -68,48 +75,145 @@ struct Operand {
     i32x4 w[KS];
 };
 
-// The keys and values of one sequence and head.
-template <int KS>
-struct Keys {
+// What the workgroup's wavefronts wrote to LDS is there, what they read is free.  (Loads
+// from global memory stay on their way.)
+__device__ __forceinline__ void meet() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Stages of KG tiles of 64 keys in LDS.  A key's row there has 4 KS units of 16 bytes; the
+// unit of channels c lies at place c ^ f(key), so that 16 lanes that read one unit of the
+// operand's 16 rows find it in 16 different columns of a 256-byte line; a channel's row
+// of values has 4 units of 16 keys, at place p ^ (channel / 4) % 4.  Units that a head of
+// d channels does not have hold others': they meet zeros of the query, or are not stored.
+// Wavefront w loads part w % RG of tile w / RG.
+template <int RG, int KG, int KS, int NV>
+struct Stage {
+    static constexpr int kKeyBytes = 4096 * KS, kValueBytes = 1024 * NV;    // of a tile
+    static constexpr int kKeyLoads = 4 * KS / RG, kValueLoads = NV / RG;    // of a wavefront
+    static_assert(kKeyLoads * RG == 4 * KS && kValueLoads * RG == NV, "parts are whole loads");
+
+    // Pages of the tile's blocks of 16 keys and the blocks' first slots in them (pages of 64
+    // keys and more: the first block's, which hold for all): uniform values, read
+    // through the scalar cache a stage ahead.
+    struct Blocks {
+        int id[4], off[4];
+    };
+
     const PagedArgs& a;
-    int b, h, len, lane;
+    int b, h, len, lane, wave;
+    bool whole;                 // a page holds whole tiles
+    int64_t head, stride;       // bytes before the head in a page, bytes of a page
 
-    // first byte of the 16 keys that hold place `at` (a multiple of 16), in k or v
-    __device__ __forceinline__ int64_t base(int at, int& off) const {
-        at = min(at, (len - 1) & ~15);          // behind the last key: its block again
-        off = at & ((1 << a.c.log2_page) - 1);
-        return head_base(a.c, page_at(a.c.table, a.c.max_pages, a.c.pages, b, at >> a.c.log2_page), h);
-    }
-
-    __device__ __forceinline__ const int8_t* k_rows(int key0) const {
-        const int m = lane & 15;
-        int off;
-        const int64_t at = base(key0 + 16 * (m >> 2), off);
-        return a.c.k + at + (int64_t)(off + (m & 3)) * a.c.d + 16 * (lane >> 4);
-    }
-
-    __device__ __forceinline__ void load_k(const int8_t* p, Operand<KS> (&k)[4]) const {
+    __device__ __forceinline__ Blocks blocks(int key0) const {
+        typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
+        const scalar_ptr table = (scalar_ptr)(a.c.table + (int64_t)b * a.c.max_pages);
+        const int tile0 = key0 + 64 * (wave / RG);
+        Blocks t;
+        if (whole) {
+            const int at = min(tile0, (len - 1) & ~63);         // behind the last tile: it again
+            t.id[0] = table[at >> a.c.log2_page];
+            t.off[0] = at & ((1 << a.c.log2_page) - 1);
+        } else {
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-                k[t].w[s] = 64 * s + 16 * (lane >> 4) < a.c.d
-                                ? *reinterpret_cast<const i32x4*>(p + 4 * t * a.c.d + 64 * s)
-                                : i32x4{0, 0, 0, 0};
-    }
-
-    // channels 16 ct + lane % 16 of the keys 16 (lane / 16) .. + 15 of the tile
-    template <int NV>
-    __device__ __forceinline__ void load_v(int key0, i32x4 (&v)[NV]) const {
-        int off;
-        const int64_t at = base(key0 + 16 * (lane >> 4), off);
-        const int page = 1 << a.c.log2_page;
-        const int8_t* p = a.c.v + at + off;
-#pragma unroll
-        for (int ct = 0; ct < NV; ++ct) {
-            const int ch = 16 * ct + (lane & 15);
-            v[ct] = ch < a.c.d ? *reinterpret_cast<const i32x4*>(p + (int64_t)ch * page) : i32x4{0, 0, 0, 0};
+            for (int p = 0; p < 4; ++p) {
+                const int at = min(tile0 + 16 * p, (len - 1) & ~15);
+                t.id[p] = table[at >> a.c.log2_page];
+                t.off[p] = at & ((1 << a.c.log2_page) - 1);
+            }
         }
+        return t;
+    }
+    // the head's first byte in a page; an id that is no page of the cache reads as page 0
+    __device__ __forceinline__ int64_t base(int id) const {
+        return head + (int64_t)((uint32_t)id < (uint32_t)a.c.pages ? id : 0) * stride;
+    }
+
+    // A stage on its way.
+    struct Loads {
+        i32x4 k[kKeyLoads], v[kValueLoads];
+    };
+
+    template <bool K, bool V>
+    __device__ __forceinline__ void load(const Blocks& t, Loads& r) const {
+        const int units = a.c.d >> 4, part = wave % RG;
+        // the lane's unit of each load, less the place of the load's first key
+        uint32_t k_at[kKeyLoads], v_at[kValueLoads];
+#pragma unroll
+        for (int i = 0; i < kKeyLoads; ++i) {
+            const int j = part * kKeyLoads + i;
+            const int row = KS == 1 ? lane >> 2 : 8 * (j & 1) + (lane >> 3);
+            const int unit = KS == 1 ? (lane & 3) ^ j : (lane & 7) ^ (((lane >> 4) & 1) | ((j >> 1) << 1));
+            k_at[i] = (uint32_t)(row * a.c.d + 16 * min(unit, units - 1));
+        }
+        const int p = (lane & 3) ^ ((lane >> 4) & 3);
+#pragma unroll
+        for (int i = 0; i < kValueLoads; ++i)
+            v_at[i] = (uint32_t)min(16 * (part * kValueLoads + i) + (lane >> 2), a.c.d - 1) << a.c.log2_page;
+        if (whole) {
+            const int64_t page = base(t.id[0]);
+            const int8_t* k = a.c.k + page + t.off[0] * a.c.d;
+            const int8_t* v = a.c.v + page + t.off[0];
+            if (K)
+#pragma unroll
+                for (int i = 0; i < kKeyLoads; ++i)
+                    r.k[i] = *reinterpret_cast<const i32x4*>(
+                        k + (k_at[i] + (uint32_t)((part * kKeyLoads + i) / KS * 16 * a.c.d)));
+            if (V)
+#pragma unroll
+                for (int i = 0; i < kValueLoads; ++i)
+                    r.v[i] = *reinterpret_cast<const i32x4*>(v + (v_at[i] + 16u * (uint32_t)p));
+        } else {
+            int64_t page[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) page[q] = base(t.id[q]);
+            if (K)
+#pragma unroll
+                for (int i = 0; i < kKeyLoads; ++i) {
+                    const int q = (part * kKeyLoads + i) / KS;
+                    const int64_t even = q & 2 ? page[2] + t.off[2] * a.c.d : page[0] + t.off[0] * a.c.d;
+                    const int64_t odd = q & 2 ? page[3] + t.off[3] * a.c.d : page[1] + t.off[1] * a.c.d;
+                    r.k[i] = *reinterpret_cast<const i32x4*>(a.c.k + (q & 1 ? odd : even) + k_at[i]);
+                }
+            if (V) {
+                const int64_t even = p & 2 ? page[2] + t.off[2] : page[0] + t.off[0];
+                const int64_t odd = p & 2 ? page[3] + t.off[3] : page[1] + t.off[1];
+                const int64_t v = p & 1 ? odd : even;
+#pragma unroll
+                for (int i = 0; i < kValueLoads; ++i)
+                    r.v[i] = *reinterpret_cast<const i32x4*>(a.c.v + v + v_at[i]);
+            }
+        }
+    }
+
+    template <bool K, bool V>
+    __device__ __forceinline__ void store(const Loads& r, int8_t* keys, int8_t* values) const {
+        const int part = wave % RG, tile = wave / RG;
+        if (K)
+#pragma unroll
+            for (int i = 0; i < kKeyLoads; ++i)
+                *reinterpret_cast<i32x4*>(keys + kKeyBytes * tile + 1024 * (part * kKeyLoads + i) + 16 * lane) = r.k[i];
+        if (V)
+#pragma unroll
+            for (int i = 0; i < kValueLoads; ++i)
+                *reinterpret_cast<i32x4*>(values + kValueBytes * tile + 1024 * (part * kValueLoads + i) + 16 * lane) = r.v[i];
+    }
+
+    __device__ __forceinline__ void read_k(const int8_t* keys, Operand<KS> (&k)[4]) const {
+        const int m = lane & 15, g = lane >> 4;
+        const int f = KS == 1 ? m >> 2 : ((m >> 1) & 1) | ((m >> 2) << 1);
+        const int8_t* p = keys + kKeyBytes * (wave / RG) + (16 * (m >> 2) + (m & 3)) * 64 * KS;
+#pragma unroll
+        for (int x = 0; x < KS; ++x)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                k[t].w[x] = *reinterpret_cast<const i32x4*>(p + 16 * ((4 * x + g) ^ f) + 256 * KS * t);
+    }
+    __device__ __forceinline__ void read_v(const int8_t* values, i32x4 (&v)[NV]) const {
+        const int m = lane & 15, g = lane >> 4;
+        const int8_t* p = values + kValueBytes * (wave / RG) + 64 * m + 16 * (g ^ (m >> 2));
+#pragma unroll
+        for (int ct = 0; ct < NV; ++ct) v[ct] = *reinterpret_cast<const i32x4*>(p + 1024 * ct);
     }
 };
 
@@ -122,7 +226,7 @@ __device__ __forceinline__ i32x4 splat(int v) { return i32x4{v, v, v, v}; }
 template <int RS, int KS>
 struct Queries {
     Operand<KS> q[RS];
-    int zp0, zp1;           // -zp_q in two terms that are bytes
+    int z0[KS], z1[KS];     // bytes of -zp_q in two terms, 0 behind the head's channels
 
     __device__ __forceinline__ void load(const PagedArgs& a, int b, int h, int row0, int rows, int lane) {
 #pragma unroll
@@ -135,41 +239,39 @@ struct Queries {
                 q[s].w[k] = at < a.c.d ? *reinterpret_cast<const i32x4*>(p + at) : i32x4{0, 0, 0, 0};
             }
         }
-        zp0 = min(-a.zp_q, 127);
-        zp1 = -a.zp_q - zp0;        // 128 = 127 + 1
+        const int zp0 = min(-a.zp_q, 127), zp1 = -a.zp_q - zp0;    // 128 = 127 + 1
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const bool in = 64 * k + 16 * (lane >> 4) < a.c.d;
+            z0[k] = in ? (zp0 & 0xFF) * 0x01010101 : 0;
+            z1[k] = in ? zp1 * 0x01010101 : 0;
+        }
     }
 
     // logits of 64 keys plus the row's `add`: acc[s][t][i] is key 16 (lane / 16) + 4 t + i
-    // of row lane % 16
+    // of row lane % 16.  SIMPLE: zp_q is not -128, and its term is taken whether it is 0 or
+    // not: the matrix cores have time, a branch would part the products from what uses them.
+    template <bool SIMPLE>
     __device__ __forceinline__ void logits(const Operand<KS> (&k)[4], const i32x4 (&add)[RS],
                                            i32x4 (&acc)[RS][4]) const {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int s = 0; s < RS; ++s) {
                 acc[s][t] = add[s];
 #pragma unroll
-                for (int x = 0; x < KS; ++x) acc[s][t] = mfma(k[t].w[x], q[s].w[x], acc[s][t]);
+                for (int x = 0; x < KS; ++x) {
+                    acc[s][t] = mfma(k[t].w[x], splat(z0[x]), acc[s][t]);
+                    if (!SIMPLE) acc[s][t] = mfma(k[t].w[x], splat(z1[x]), acc[s][t]);
+                    acc[s][t] = mfma(k[t].w[x], q[s].w[x], acc[s][t]);
+                }
             }
-        }
-        if (zp0) {
-            const i32x4 z0 = splat((zp0 & 0xFF) * 0x01010101), z1 = splat(zp1 * 0x01010101);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int s = 0; s < RS; ++s)
-#pragma unroll
-                    for (int x = 0; x < KS; ++x) {
-                        acc[s][t] = mfma(k[t].w[x], z0, acc[s][t]);
-                        if (zp1) acc[s][t] = mfma(k[t].w[x], z1, acc[s][t]);
-                    }
-        }
     }
 };
 
-// Whether a row of this limit sees key 4 t + i of the lane's 16 keys of a tile.
-__device__ __forceinline__ bool seen(int key0, int t, int i, int limit, int lane) {
-    return key0 + 16 * (lane >> 4) + 4 * t + i < limit;
+// How many of the lane's 16 keys of a tile a row of this limit sees (the first ones).
+__device__ __forceinline__ int seen(int key0, int limit, int lane) {
+    return min(max(limit - (key0 + 16 * (lane >> 4)), 0), 16);
 }
 
 // ---------------------------------------------------------------------------
@@ -177,27 +279,28 @@ __device__ __forceinline__ bool seen(int key0, int t, int i, int limit, int lane
 // ---------------------------------------------------------------------------
 
 // U_k: the least u in [0, n d] with c_k e(u) <= 2 S; n d + 1 where there is none.
-// With u = z d + rho, e = ((q_b - rho)^2 + q_c) 2^(n - z): the octave z is the first whose
-// last value satisfies it, the place in it an integer square root.
-__device__ int threshold(uint64_t S2, int k, const LisConsts& c) {
+// With u = z d + rho, e = q_L(rho) 2^(n - z), q_L(rho) = (q_b - rho)^2 + q_c: the octave z is
+// the first whose last value satisfies it, n - z = floor(log2(2 S / (c_k q_L(d - 1)))),
+// settled by one comparison.  In it q_b - rho = floor(sqrt(X / c_k - q_c)), X =
+// floor(2 S / 2^(n - z)): from binary32 values that come within 2^-9 of it (q_L below
+// 2^24, c_k below 2^16: three roundings), so that the next integer is tried, exactly.
+__device__ __forceinline__ int threshold(uint64_t S2, int k, const LisConsts& c) {
     const uint32_t ck = k == 1 ? 3u : (3u << (k - 1)) - 1u;
     const uint32_t wl = c.qb - c.d_ln2 + 1, last = wl * wl + c.qc, first = c.qb * c.qb + c.qc;
-    const auto fits = [&](int z) { return (uint64_t)last * ck <= (S2 >> (c.n - z)); };
-    // an estimate of z, then exactly
-    const float f = (float)S2 / ((float)last * (float)ck);
-    int z = min(max(c.n - ((int)(__float_as_uint(f) >> 23) - 127), 0), c.n);
-    while (z < c.n && !fits(z)) ++z;
-    while (z > 0 && fits(z - 1)) --z;
+    const uint64_t Q = (uint64_t)last * ck;
+    int j = __clzll((long long)Q) - __clzll((long long)S2);         // msb(S2) - msb(Q)
+    j = j >= 0 && (Q << j) > S2 ? j - 1 : j;
+    const int z = c.n - min(max(j, 0), c.n);
     const uint64_t X = S2 >> (c.n - z);
-    if (z == c.n) return (uint64_t)first * ck <= X ? c.n * (int)c.d_ln2 : c.n * (int)c.d_ln2 + 1;
+    const int none = c.n * (int)c.d_ln2 + 1;
+    // the first value of the octave (of the last one, z = n, there is no other)
     if ((uint64_t)first * ck <= X) return z * (int)c.d_ln2;
-    // (q_b - rho)^2 <= floor(X / c_k) - q_c; X < first c_k < 2^40, and X / c_k lies at
-    // least 1 / c_k below the next integer: its binary64 quotient has the right floor
-    const uint32_t y = (uint32_t)((double)X / (double)ck) - c.qc;
-    uint32_t w = (uint32_t)sqrtf((float)y);
-    while (w * w > y) --w;
-    while ((w + 1) * (w + 1) <= y) ++w;
-    return z * (int)c.d_ln2 + (int)(c.qb - w);
+    if (z == c.n) return none;
+    float w = (float)X * __builtin_amdgcn_rcpf((float)ck) - (float)c.qc;
+    w = __builtin_amdgcn_sqrtf(fmaxf(w, 0.0f));
+    uint32_t i = (uint32_t)(w + 0.5f);      // floor or one more
+    if (((uint64_t)(i * i + c.qc)) * ck > X) --i;
+    return z * (int)c.d_ln2 + (int)(c.qb - i);
 }
 
 // The words of a row's buckets, by the threads of a workgroup: bucket j >= 1 holds
@@ -225,34 +328,27 @@ __device__ __forceinline__ void fill_buckets(const int* U, int k, int top, int s
 // Exact row sum from values e 2^-n held in binary32: the 16 values of a tile are added
 // in binary64 to 2^(52 - n), whose unit is 2^-n; the sum's low bits are then their sum
 // as an integer (16 2^24 2^n < 2^52: n <= 23; deeper clamps take the general path).
-template <bool FAST>
+template <Mode MODE>
 struct RowAdder {
     uint64_t sum = 0;
 
-    // P0: the I-Exp needs no pre-shift (q_ln2 above 512)
-    template <bool P0>
-    __device__ __forceinline__ void fast(const i32x4 (&acc)[4], const PagedArgs& a, bool edge, int key0,
-                                         int limit, int lane) {
-        const double unit = __longlong_as_double((int64_t)(1023 + 52 - a.k.n) << 52);
-        double s0 = unit, s1 = unit;
+    // a key that is not seen holds the lowest value here, is clamped to e = q_L(0) 2^-n, and
+    // `unseen` of them are taken off again
+    __device__ __forceinline__ void add(const i32x4 (&acc)[4], int mx, const PagedArgs& a) {
+        if constexpr (MODE != kGeneral) {
+            const double unit = __longlong_as_double((int64_t)(1023 + 52 - a.k.n) << 52);
+            double s0 = unit, s1 = unit;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t e = lis::screen_iexp<P0>(acc[t][i], 0, a.k);       // the row's offset is in acc
-                if (edge) e = seen(key0, t, i, limit, lane) ? e : 0u;
-                if (i & 1) s1 += (double)__uint_as_float(e);
-                else s0 += (double)__uint_as_float(e);
-            }
-        const uint64_t m = (1ull << 52) - 1;
-        sum += ((uint64_t)__double_as_longlong(s0) & m) + ((uint64_t)__double_as_longlong(s1) & m);
-    }
-
-    __device__ __forceinline__ void add(const i32x4 (&acc)[4], int mx, const PagedArgs& a, bool edge,
-                                        int key0, int limit, int lane) {
-        if constexpr (FAST) {
-            if (a.k.s_pre == 0) fast<true>(acc, a, edge, key0, limit, lane);
-            else fast<false>(acc, a, edge, key0, limit, lane);
+                for (int i = 0; i < 4; ++i) {
+                    // the row's offset is in acc
+                    const uint32_t e = lis::screen_iexp<MODE == kPlain>(acc[t][i], 0, a.k);
+                    if (i & 1) s1 += (double)__uint_as_float(e);
+                    else s0 += (double)__uint_as_float(e);
+                }
+            const uint64_t m = (1ull << 52) - 1;
+            sum += ((uint64_t)__double_as_longlong(s0) & m) + ((uint64_t)__double_as_longlong(s1) & m);
         } else {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -260,9 +356,12 @@ struct RowAdder {
                 for (int i = 0; i < 4; ++i) {
                     uint32_t z;
                     const uint32_t qL = lis::iexp_qL(acc[t][i], mx, a.k, z);
-                    sum += !edge || seen(key0, t, i, limit, lane) ? (uint64_t)qL << (a.k.n - (int)z) : 0;
+                    sum += (uint64_t)qL << (a.k.n - (int)z);
                 }
         }
+    }
+    __device__ __forceinline__ void take_off(int unseen, const PagedArgs& a) {
+        sum -= (uint64_t)unseen * (a.k.qb * a.k.qb + a.k.qc);
     }
 };
 
@@ -271,33 +370,60 @@ __device__ __forceinline__ uint32_t top_bytes(uint32_t x0, uint32_t x1, uint32_t
     return __builtin_amdgcn_perm(x1, x0, 0x0c0c0703u) | __builtin_amdgcn_perm(x3, x2, 0x07030c0cu);
 }
 
-// Four weights 2^m from the bytes m: their operands hi and lo.
-__device__ __forceinline__ void digits(uint32_t m, uint32_t& hi, uint32_t& lo) {
+// Four weights 2^m from the bytes m: their operands hi and lo; 0 where `keep` has no bits.
+__device__ __forceinline__ void digits(uint32_t m, uint32_t keep, uint32_t& hi, uint32_t& lo) {
     const uint32_t v = __builtin_amdgcn_perm(0x80C0E0F0u, 0xF8FCFEFFu, m & 0x07070707u);
     const uint32_t up = __builtin_amdgcn_perm(0u, 0x0000FF00u, (m >> 3) & 0x01010101u);
-    hi = v & up;
-    lo = v & ~up;
+    hi = v & up & keep;
+    lo = v & ~up & keep;
 }
 
-template <int RS, int KS, int NV, Pass PASS, bool STORED, bool FAST, bool WEIGHT>
-__global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape sh) {
-    constexpr int kRows = 16 * RS;
+// Maxima of the rows over all parts, a wavefront a row.
+__device__ __forceinline__ void parts_max(const Shape& sh, int64_t row_at, int rows, int lane, int wave,
+                                          int waves, int* row_max) {
+    for (int r = wave; r < rows; r += waves) {
+        int m = INT_MIN;
+        for (int i = lane; i < sh.splits; i += 64) m = max(m, sh.part_max[(row_at + r) * sh.splits + i]);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) m = max(m, __shfl_xor(m, o));
+        if (lane == 0) row_max[r] = m;
+    }
+}
+
+template <int RS_, int RG_, int KG_, int KS_, int NV_>
+struct Config {
+    static constexpr int RS = RS_;          // sets of 16 rows of a wavefront
+    static constexpr int RG = RG_, KG = KG_;    // row groups, key groups: RG KG wavefronts
+    static constexpr int KS = KS_, NV = NV_;    // 64-byte steps and 16-channel tiles of a head
+    static constexpr int threads = 64 * RG * KG, rows = 16 * RS * RG;
+};
+
+template <class C, Pass PASS, bool STORED, Mode MODE, bool WEIGHT>
+__global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, Shape sh) {
+    constexpr int RS = C::RS, RG = C::RG, KG = C::KG, KS = C::KS, NV = C::NV;
+    constexpr int kBlock = C::threads, tile_rows = C::rows, kRows = 16 * RS;
+    constexpr bool FAST = MODE != kGeneral;
+    constexpr bool KEYS = !(STORED && PASS == kOut), VALUES = PASS == kAll || PASS == kOut;
+    typedef Stage<RG, KG, KS, NV> St;
+    // two stages
+    constexpr int kK = KEYS ? KG * St::kKeyBytes : 16, kV = VALUES ? KG * St::kValueBytes : 16;
+    __shared__ __attribute__((aligned(16))) int8_t stage_k[2][kK], stage_v[2][kV];
     extern __shared__ uint32_t dyn[];               // buckets, then the workgroup's out
-    __shared__ int row_max[kRows * kWaves];
-    __shared__ unsigned long long row_sum[kRows * kWaves];
-    __shared__ int U[kRows * kWaves][kMaxTop];
+    __shared__ int row_max[tile_rows];
+    __shared__ unsigned long long row_sum[tile_rows];
+    __shared__ int U[VALUES && FAST ? tile_rows : 1][kMaxTop];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int RG = sh.row_groups, KG = kWaves / RG;
-    const int rg = wave / KG, kg = wave - rg * KG;
-    const int tile_rows = RG * kRows;
+    const int rg = wave % RG, kg = wave / RG;
     // fewer than 2^24 workgroups: 32-bit divisions
     const uint32_t block = (uint32_t)lis::xcd_remap(blockIdx.x, gridDim.x);
     const uint32_t wg = block / (uint32_t)sh.splits;
     const int split = (int)(block - wg * (uint32_t)sh.splits);
     const int64_t unit = wg / (uint32_t)sh.tiles;
-    const int tile = sh.tiles - 1 - (int)(wg - (uint32_t)unit * (uint32_t)sh.tiles);    // the rows that see most come first
-    const int b = (int)((uint32_t)unit / (uint32_t)a.c.Hkv), h = (int)unit - b * a.c.Hkv;
+    // the rows that see most come first
+    const int tile = sh.tiles - 1 - (int)(wg - (uint32_t)unit * (uint32_t)sh.tiles);
+    // heads first: the workgroups of an XCD, which are neighbours, see several sequences
+    const int h = (int)((uint32_t)unit / (uint32_t)a.c.B), b = (int)unit - h * a.c.B;
     const int len = keys_of(a.c, b);
     const int fresh = a.n_new ? min(max(a.n_new[b], 0), a.L) : a.L;
     const int rows = fresh * a.group;
@@ -309,41 +435,107 @@ __global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape
     int limit[RS];
 #pragma unroll
     for (int s = 0; s < RS; ++s) limit[s] = limit_of(a, len, fresh, min(row0 + 16 * s + (lane & 15), rows - 1));
-    // keys that some row of the wavefront sees, that every one does, and that some row of the workgroup does
+    // keys that every row of the wavefront sees, and that some row of the workgroup does
     const int full = limit_of(a, len, fresh, min(row0, rows - 1));
     const int all = limit_of(a, len, fresh, min(first + tile_rows, rows) - 1);
     const int per = ((all + kTile - 1) / kTile + sh.splits - 1) / sh.splits * kTile;
-    const int from = min(split * per, all);
-    const int to = idle ? 0 : min(from + per, limit_of(a, len, fresh, min(row0 + kRows, rows) - 1));
-    const int key_first = from + kg * kTile, key_step = KG * kTile;
+    const int from = min(split * per, all), until = min(from + per, all);
+    const int to = idle ? 0 : min(until, limit_of(a, len, fresh, min(row0 + kRows, rows) - 1));
+    const int whole = min(full, to);                // tiles that end here or before are seen whole
+    const int stages = (until - from + KG * kTile - 1) / (KG * kTile);
 
     Queries<RS, KS> q;
-    const Keys<KS> keys{a, b, h, len, lane};
-    if (!STORED || PASS != kOut) q.load(a, b, h, min(row0, rows - 1), rows, lane);
+    const int64_t head_bytes = (int64_t)a.c.d << a.c.log2_page;
+    const St st{a, b, h, len, lane, wave, a.c.log2_page >= 6, h * head_bytes, a.c.Hkv * head_bytes};
+    if (KEYS) q.load(a, b, h, min(row0, rows - 1), rows, lane);
     int32_t* lg = nullptr;
     if (STORED) lg = sh.logits + (unit * sh.rows + min(lane & 15, sh.rows - 1)) * sh.keys + 16 * (lane >> 4);
 
-    // body(key0, logits + add, edge) for each of the wavefront's tiles
-    const auto walk = [&](const i32x4 (&add)[RS], auto&& body) {
-        if (key_first >= to) return;
-        Operand<KS> k[4];
-        const int8_t* next = keys.k_rows(key_first);
-        keys.load_k(next, k);
-        next = keys.k_rows(key_first + key_step);
-        for (int key0 = key_first; key0 < to; key0 += key_step) {
-            Operand<KS> kn[4];
-            keys.load_k(next, kn);
-            next = keys.k_rows(key0 + 2 * key_step);
-            i32x4 acc[RS][4];
-            q.logits(k, add, acc);
-            body(key0, acc, key0 + kTile > full);
+    // body(key0, logits + add, values, edge) for each of the wavefront's tiles.  edge: a row
+    // may not see all of it; the logits that it does not see are the lowest value.  What
+    // a branch on this holds is kept to a few registers, so that the passes' sums stay
+    // where they are.
+    constexpr int step = KG * kTile;
+    typename St::Loads r[2];
+    typename St::Blocks next;
+    // the first two stages on their way
+    const auto prime = [&](auto with_values) {
+        constexpr bool V = decltype(with_values)::value;
+        if (stages == 0) return;
+        next = st.blocks(from);
+        st.template load<KEYS, V>(next, r[0]);
+        next = st.blocks(from + step);
+        st.template load<KEYS, V>(next, r[1]);
+        next = st.blocks(from + 2 * step);
+    };
+    const auto walk = [&](const i32x4 (&add)[RS], auto with_values, auto&& body) {
+        constexpr bool V = decltype(with_values)::value;
+        if (stages == 0) return;
+        const int own = from + kg * kTile;
+        st.template store<KEYS, V>(r[0], stage_k[0], stage_v[0]);
+        st.template load<KEYS, V>(next, r[0]);
+        next = st.blocks(from + 3 * step);
+        meet();
+        const auto stored = [&](int key0, i32x4 (&acc)[RS][4]) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) k[t] = kn[t];
-        }
+            for (int t = 0; t < 4; ++t)
+                acc[0][t] = *reinterpret_cast<const i32x4*>(lg + min(key0, (int)sh.keys - kTile) + 4 * t);
+        };
+        i32x4 ahead[RS][4];
+        if (!KEYS) stored(own, ahead);
+        // stage n, of parity i: stage n + 1 goes into LDS, stage n + 3 is sent for
+        const auto stage = [&](int n, auto i_, auto works) {
+            constexpr int i = decltype(i_)::value;
+            const int key0 = own + n * step;
+            i32x4 acc[RS][4];
+            st.template store<KEYS, V>(r[i ^ 1], stage_k[i ^ 1], stage_v[i ^ 1]);
+            if (!KEYS) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[0][t] = ahead[0][t];
+                stored(key0 + step, ahead);
+            }
+            st.template load<KEYS, V>(next, r[i ^ 1]);
+            next = st.blocks(from + (n + 4) * step);
+            if (decltype(works)::value) {
+                if (KEYS) {
+                    Operand<KS> k[4];
+                    st.read_k(stage_k[i], k);
+                    q.template logits<FAST>(k, add, acc);
+                } else {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) acc[0][t] += add[0];
+                }
+                const bool edge = key0 + kTile > whole;
+                if (edge) {
+#pragma unroll
+                    for (int s = 0; s < RS; ++s) {
+                        const int n_seen = seen(key0, min(limit[s], to), lane);
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) acc[s][t][x] = 4 * t + x < n_seen ? acc[s][t][x] : INT_MIN;
+                    }
+                }
+                body(key0, acc, stage_v[i], edge);
+            }
+            meet();
+        };
+        const auto turns = [&](auto works) {
+            int n = 0;
+            for (; n + 2 <= stages; n += 2) {
+                stage(n, std::integral_constant<int, 0>{}, works);
+                stage(n + 1, std::integral_constant<int, 1>{}, works);
+            }
+            if (n < stages) stage(n, std::integral_constant<int, 0>{}, works);
+        };
+        if (idle) turns(std::false_type{});     // no rows of its own: it loads for the others
+        else turns(std::true_type{});
     };
 
-    const int64_t part0 = ((unit * sh.tiles + tile) * sh.splits) * tile_rows;
+    // the workgroup's rows in the workspace
+    const int64_t row_at = (unit * sh.tiles + tile) * tile_rows;
     i32x4 add[RS];
+    prime(std::integral_constant<bool, PASS == kOut>{});
 
     // --- maximum
     for (int i = threadIdx.x; i < tile_rows; i += kBlock) {
@@ -358,19 +550,13 @@ __global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape
             mx[s] = INT_MIN;
             add[s] = splat(0);
         }
-        walk(add, [&](int key0, const i32x4 (&acc)[RS][4], bool edge) {
+        walk(add, std::false_type{}, [&](int key0, const i32x4 (&acc)[RS][4], const int8_t*, bool) {
 #pragma unroll
             for (int s = 0; s < RS; ++s)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    if (!edge) {
-                        mx[s] = max(max(max(mx[s], acc[s][t][0]), acc[s][t][1]), max(acc[s][t][2], acc[s][t][3]));
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            mx[s] = max(mx[s], seen(key0, t, i, limit[s], lane) ? acc[s][t][i] : INT_MIN);
-                    }
-                    if (STORED && s == 0 && (lane & 15) < sh.rows)
+                    mx[s] = max(max(max(mx[s], acc[s][t][0]), acc[s][t][1]), max(acc[s][t][2], acc[s][t][3]));
+                    if (STORED && (lane & 15) < sh.rows && key0 < to)
                         *reinterpret_cast<i32x4*>(lg + key0 + 4 * t) = acc[s][t];
                 }
         });
@@ -381,19 +567,31 @@ __global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape
         }
         __syncthreads();
         if (PASS == kMax) {
-            for (int i = threadIdx.x; i < tile_rows; i += kBlock)
-                sh.part_max[part0 + (int64_t)split * tile_rows + i] = row_max[i];
-            if (split == 0)         // the parts of the last pass add to it
-                for (int at = threadIdx.x; at < tile_rows * (a.c.d >> 2); at += kBlock) {
-                    const int r = at / (a.c.d >> 2), ch = at - r * (a.c.d >> 2);
-                    if (first + r < rows)
-                        *reinterpret_cast<i32x4*>(a.out + query_of(a, b, h, first + r) * a.c.d + 4 * ch) = splat(0);
+            for (int i = threadIdx.x; i < tile_rows; i += kBlock) {
+                sh.part_max[(row_at + i) * sh.splits + split] = row_max[i];
+                if (split == 0) sh.row_sum[row_at + i] = 0;     // the parts of the next pass add to it
+            }
+            if (split == 0 && kg == 0)      // and those of the last one to out
+#pragma unroll
+                for (int s = 0; s < RS; ++s) {
+                    const int rho = row0 + 16 * s + (lane & 15);
+                    if (rho >= rows) continue;
+                    int32_t* out = a.out + query_of(a, b, h, rho) * a.c.d;
+                    for (int ch = 4 * (lane >> 4); ch < a.c.d; ch += 16)
+                        *reinterpret_cast<i32x4*>(out + ch) = splat(0);
                 }
             return;
         }
+    } else if (PASS == kSum) {
+        parts_max(sh, row_at, min(tile_rows, rows - first), lane, wave, C::threads / 64, row_max);
+        __syncthreads();
+        if (split == 0)
+            for (int i = threadIdx.x; i < tile_rows; i += kBlock) sh.row_max[row_at + i] = row_max[i];
     } else {
-        for (int at = threadIdx.x; at < tile_rows * sh.splits; at += kBlock)
-            atomicMax(&row_max[at % tile_rows], sh.part_max[part0 + at]);
+        for (int i = threadIdx.x; i < tile_rows; i += kBlock) {
+            row_max[i] = sh.row_max[row_at + i];
+            row_sum[i] = sh.row_sum[row_at + i];
+        }
         __syncthreads();
     }
 
@@ -402,15 +600,16 @@ __global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape
 #pragma unroll
     for (int s = 0; s < RS; ++s) mx[s] = row_max[rg * kRows + 16 * s + (lane & 15)];
     if (PASS == kAll || PASS == kSum) {
-        RowAdder<FAST> sum[RS];
+        if (PASS == kAll) prime(std::false_type{});
+        RowAdder<MODE> sum[RS];
 #pragma unroll
         for (int s = 0; s < RS; ++s) add[s] = splat(FAST ? -lis::screen_c(mx[s], a.k) : 0);
-        walk(add, [&](int key0, const i32x4 (&acc)[RS][4], bool edge) {
+        walk(add, std::false_type{}, [&](int key0, const i32x4 (&acc)[RS][4], const int8_t*, bool edge) {
 #pragma unroll
-            for (int s = 0; s < RS; ++s) {
-                if (edge) sum[s].add(acc[s], mx[s], a, true, key0, limit[s], lane);
-                else sum[s].add(acc[s], mx[s], a, false, key0, limit[s], lane);
-            }
+            for (int s = 0; s < RS; ++s) sum[s].add(acc[s], mx[s], a);
+            if (edge)
+#pragma unroll
+                for (int s = 0; s < RS; ++s) sum[s].take_off(16 - seen(key0, min(limit[s], to), lane), a);
         });
 #pragma unroll
         for (int s = 0; s < RS; ++s) {
@@ -420,21 +619,13 @@ __global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape
         __syncthreads();
         if (PASS == kSum) {
             for (int i = threadIdx.x; i < tile_rows; i += kBlock)
-                sh.part_sum[part0 + (int64_t)split * tile_rows + i] = row_sum[i];
+                atomicAdd(reinterpret_cast<unsigned long long*>(sh.row_sum) + row_at + i, row_sum[i]);
             return;
         }
-    } else {
-        for (int at = threadIdx.x; at < tile_rows * sh.splits; at += kBlock)
-            atomicAdd(&row_sum[at % tile_rows], (unsigned long long)sh.part_sum[part0 + at]);
-        __syncthreads();
     }
 
     // --- thresholds
-    const int out_at = FAST ? tile_rows * sh.buckets : 0;
-    const bool shared_out = KG > 1 || PASS == kOut;
-    int32_t* wg_out = reinterpret_cast<int32_t*>(dyn + out_at);
-    if (shared_out)
-        for (int i = threadIdx.x; i < tile_rows * a.c.d; i += kBlock) wg_out[i] = 0;
+    if (PASS == kAll) prime(std::true_type{});
     lis::RowSum rs[RS];
     if (FAST) {
         for (int at = threadIdx.x; at < tile_rows * a.k.top; at += kBlock) {
@@ -459,9 +650,9 @@ __global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape
     i32x4 hi[RS][NV] = {}, lo[RS][NV] = {}, ph[RS] = {}, pl[RS] = {};
     const i32x4 ones = splat(0x01010101);
     const int cap = min(a.k.n, a.k.top) * (int)a.k.d_ln2;
-    const auto product = [&](int key0, const i32x4 (&acc)[RS][4], bool edge) {
+    const auto product = [&](int key0, const i32x4 (&acc)[RS][4], const int8_t* values, bool edge) {
         i32x4 v[NV];
-        keys.load_v(key0, v);
+        st.read_v(values, v);
 #pragma unroll
         for (int s = 0; s < RS; ++s) {
             uint32_t m[4];
@@ -484,19 +675,20 @@ __global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape
                 }
                 m[t] = top_bytes(x[0], x[1], x[2], x[3]);
             }
+            i32x4 keep = splat(-1);
+            if (edge) {
+                const int n_seen = seen(key0, min(limit[s], to), lane);
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (4 * t + i >= n_seen) keep[t] &= ~(0xFF << (8 * i));
+            }
             i32x4 wh, wl;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 uint32_t dh, dl;
-                digits(m[t], dh, dl);
-                if (edge) {
-                    uint32_t keep = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        keep |= seen(key0, t, i, limit[s], lane) ? 0xFFu << (8 * i) : 0u;
-                    dh &= keep;
-                    dl &= keep;
-                }
+                digits(m[t], (uint32_t)keep[t], dh, dl);
                 wh[t] = (int)dh;
                 wl[t] = (int)dl;
             }
@@ -505,10 +697,9 @@ __global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape
                 hi[s][ct] = mfma(v[ct], wh, hi[s][ct]);
                 lo[s][ct] = mfma(v[ct], wl, lo[s][ct]);
             }
-            if (a.zp_v) {
-                ph[s] = mfma(ones, wh, ph[s]);
-                pl[s] = mfma(ones, wl, pl[s]);
-            }
+            // sums of the weights, for zp_v: cheaper than a branch on it
+            ph[s] = mfma(ones, wh, ph[s]);
+            pl[s] = mfma(ones, wl, pl[s]);
             if (WEIGHT) {
                 const bool mine = row0 + 16 * s + (lane & 15) < rows;
 #pragma unroll
@@ -532,21 +723,30 @@ __global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape
     };
 #pragma unroll
     for (int s = 0; s < RS; ++s) add[s] = splat(FAST ? -mx[s] : 0);
-    if (STORED && PASS == kOut) {
-        for (int key0 = key_first; key0 < to; key0 += key_step) {
-            i32x4 acc[RS][4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                acc[0][t] = *reinterpret_cast<const i32x4*>(lg + key0 + 4 * t);
-                if (FAST) acc[0][t] += add[0];
-            }
-            product(key0, acc, key0 + kTile > full);
-        }
-    } else {
-        walk(add, product);
-    }
+    walk(add, std::true_type{}, product);
 
-    // --- out
+    // --- out: what the wavefronts of the other key groups hold comes to the first one's
+#pragma unroll
+    for (int s = 0; s < RS; ++s)
+#pragma unroll
+        for (int ct = 0; ct < NV; ++ct)
+            lo[s][ct] = a.zp_v * (ph[s] * 256 + pl[s]) - (hi[s][ct] * 256 + lo[s][ct]);
+    if (KG > 1) {
+        i32x4* held = reinterpret_cast<i32x4*>(dyn + (FAST ? tile_rows * sh.buckets : 0));
+        if (kg > 0)
+#pragma unroll
+            for (int s = 0; s < RS; ++s)
+#pragma unroll
+                for (int ct = 0; ct < NV; ++ct)
+                    held[(((kg - 1) * RG + rg) * RS * NV + s * NV + ct) * 64 + lane] = lo[s][ct];
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int s = 0; s < RS; ++s)
+#pragma unroll
+            for (int ct = 0; ct < NV; ++ct)
+                for (int g = 0; g + 1 < KG; ++g) lo[s][ct] += held[((g * RG + rg) * RS * NV + s * NV + ct) * 64 + lane];
+    }
 #pragma unroll
     for (int s = 0; s < RS; ++s) {
         const int rho = row0 + 16 * s + (lane & 15);
@@ -556,26 +756,13 @@ __global__ __launch_bounds__(kBlock, 2) void lis_paged_kernel(PagedArgs a, Shape
         for (int ct = 0; ct < NV; ++ct) {
             const int ch = 16 * ct + 4 * (lane >> 4);
             if (ch >= a.c.d) continue;
-            i32x4 o;
+            if (PASS == kOut) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                o[i] = a.zp_v * (ph[s][i] * 256 + pl[s][i]) - (hi[s][ct][i] * 256 + lo[s][ct][i]);
-            if (shared_out) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) atomicAdd(&wg_out[(rho - first) * a.c.d + ch + i], o[i]);
+                for (int i = 0; i < 4; ++i) atomicAdd(out + ch + i, lo[s][ct][i]);
             } else {
-                *reinterpret_cast<i32x4*>(out + ch) = o;
+                *reinterpret_cast<i32x4*>(out + ch) = lo[s][ct];
             }
         }
-    }
-    if (!shared_out) return;
-    __syncthreads();
-    for (int at = threadIdx.x; at < tile_rows * a.c.d; at += kBlock) {
-        const int r = at / a.c.d, ch = at - r * a.c.d;
-        if (first + r >= rows) break;
-        int32_t* out = a.out + query_of(a, b, h, first + r) * a.c.d + ch;
-        if (PASS == kOut) atomicAdd(out, wg_out[at]);
-        else *out = wg_out[at];
     }
 }
 
@@ -589,7 +776,7 @@ __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shap
     const uint32_t block = (uint32_t)lis::xcd_remap(blockIdx.x, gridDim.x);
     const int64_t unit = block / (uint32_t)sh.splits;
     const int split = (int)(block - (uint32_t)unit * (uint32_t)sh.splits);
-    const int b = (int)((uint32_t)unit / (uint32_t)a.c.Hkv);
+    const int b = (int)((uint32_t)unit % (uint32_t)a.c.B);
     const int len = keys_of(a.c, b);
     const int fresh = a.n_new ? min(max(a.n_new[b], 0), a.L) : a.L;
     const int rows = fresh * a.group;
@@ -597,17 +784,13 @@ __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shap
     const int all = limit_of(a, len, fresh, rows - 1);
     const int per = ((all + kTile - 1) / kTile + sh.splits - 1) / sh.splits * kTile;
     const int from = min(split * per, all), to = min(from + per, all);
-    const int64_t part0 = unit * sh.splits * 16;
-    if (threadIdx.x < 16) {
-        row_max[threadIdx.x] = INT_MIN;
-        row_sum[threadIdx.x] = 0;
-    }
+    const int64_t row_at = unit * 16;
+    if (threadIdx.x < 16) row_sum[threadIdx.x] = 0;
+    parts_max(sh, row_at, rows, lane, wave, kBlock / 64, row_max);
     __syncthreads();
-    for (int at = threadIdx.x; at < 16 * sh.splits; at += kBlock)
-        atomicMax(&row_max[at % 16], sh.part_max[part0 + at]);
-    __syncthreads();
+    if (split == 0 && threadIdx.x < rows) sh.row_max[row_at + threadIdx.x] = row_max[threadIdx.x];
     const int runs = (to - from + 255) / 256;
-    for (int at = wave; at < rows * runs; at += kWaves) {
+    for (int at = wave; at < rows * runs; at += kBlock / 64) {
         const int r = at / runs, key0 = from + 256 * (at - r * runs) + 4 * lane;
         const int end = min(to, limit_of(a, len, fresh, r));
         uint64_t sum = 0;
@@ -634,7 +817,8 @@ __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shap
         if (lane == 0) atomicAdd(&row_sum[r], (unsigned long long)sum);
     }
     __syncthreads();
-    if (threadIdx.x < 16) sh.part_sum[part0 + (int64_t)split * 16 + threadIdx.x] = row_sum[threadIdx.x];
+    if (threadIdx.x < rows)
+        atomicAdd(reinterpret_cast<unsigned long long*>(sh.row_sum) + row_at + threadIdx.x, row_sum[threadIdx.x]);
 }
 
 // ---------------------------------------------------------------------------
@@ -643,81 +827,85 @@ __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shap
 
 // Whether the thresholds and the binary32 I-Exp hold for these constants: q_L below
 // 2^24 (which keeps d below 2^11), e(u) not increasing over an octave's end, buckets of
-// at least 8 values, and the sums of a tile below 2^52.
-bool fast_path(const LisConsts& k) {
+// at least 8 values, the sums of a tile below 2^52, and -zp_q a byte.
+Mode mode_of(const PagedArgs& a) {
+    const LisConsts& k = a.k;
     const uint64_t first = (uint64_t)k.qb * k.qb + k.qc;
     const uint64_t w = k.qb - k.d_ln2 + 1, last = w * w + k.qc;
-    return first < (1u << 24) && 2 * last >= first && k.d_ln2 >= 16 && k.n <= 23;
+    if (first >= (1u << 24) || 2 * last < first || k.d_ln2 < 16 || k.n > 23 || a.zp_q == -128) return kGeneral;
+    return k.s_pre ? kShifted : kPlain;
 }
 
-template <int RS, int KS, int NV, Pass PASS, bool STORED>
-void enqueue(const PagedArgs& a, const Shape& sh, const Plan& p, bool fast, hipStream_t stream) {
-    const bool last = PASS == kAll || PASS == kOut;
-    const bool shared_out = last && (p.row_groups < kWaves || PASS == kOut);
-    const size_t lds = 4 * ((last && fast ? (size_t)p.tile_rows() * sh.buckets : 0) +
-                            (shared_out ? (size_t)p.tile_rows() * a.c.d : 0));
-    constexpr bool kWeight = PASS == kAll || PASS == kOut;
-    const bool weight = kWeight && a.c.weight;
-    launch_kernel(fast ? (weight ? lis_paged_kernel<RS, KS, NV, PASS, STORED, true, kWeight>
-                                 : lis_paged_kernel<RS, KS, NV, PASS, STORED, true, false>)
-                       : (weight ? lis_paged_kernel<RS, KS, NV, PASS, STORED, false, kWeight>
-                                 : lis_paged_kernel<RS, KS, NV, PASS, STORED, false, false>),
-                  dim3((uint32_t)(p.units * p.tiles * p.splits)), dim3(kBlock), lds, stream, a, sh);
+template <class C, Pass PASS, bool STORED>
+void enqueue(const PagedArgs& a, const Shape& sh, const Plan& p, hipStream_t stream) {
+    constexpr bool last = PASS == kAll || PASS == kOut;
+    const Mode mode = mode_of(a);
+    const size_t lds = last ? 4 * (mode != kGeneral ? (size_t)C::rows * sh.buckets : 0) +
+                                  (size_t)(C::KG - 1) * C::RG * C::RS * C::NV * 1024
+                            : 0;
+    const bool weight = last && a.c.weight;
+    const auto kernel =
+        mode == kPlain ? (weight ? lis_paged_kernel<C, PASS, STORED, kPlain, last>
+                                 : lis_paged_kernel<C, PASS, STORED, kPlain, false>)
+        : mode == kShifted ? (weight ? lis_paged_kernel<C, PASS, STORED, kShifted, last>
+                                     : lis_paged_kernel<C, PASS, STORED, kShifted, false>)
+                           : (weight ? lis_paged_kernel<C, PASS, STORED, kGeneral, last>
+                                     : lis_paged_kernel<C, PASS, STORED, kGeneral, false>);
+    launch_kernel(kernel, dim3((uint32_t)(p.units * p.tiles * p.splits)), dim3(C::threads), lds, stream, a, sh);
 }
 
-// RS: sets of rows a wavefront holds where there are more than 16 rows
-template <int RS, int KS, int NV>
+// CHUNK: more than 16 rows; FEW: up to 16.
+template <class CHUNK, class FEW>
 void launch(const PagedArgs& a, const Shape& sh, const Plan& p, hipStream_t stream) {
-    const bool fast = fast_path(a.k);
     if (p.splits == 1) {
-        if (p.sets == 1) enqueue<1, KS, NV, kAll, false>(a, sh, p, fast, stream);
-        else enqueue<RS, KS, NV, kAll, false>(a, sh, p, fast, stream);
+        if (p.rows <= 16) enqueue<FEW, kAll, false>(a, sh, p, stream);
+        else enqueue<CHUNK, kAll, false>(a, sh, p, stream);
         return;
     }
     const LaunchEvents ev = launch_events();
     set_launch_events(ev.start, nullptr);
-    if (p.stored) enqueue<1, KS, NV, kMax, true>(a, sh, p, fast, stream);
-    else enqueue<RS, KS, NV, kMax, false>(a, sh, p, fast, stream);
+    if (p.stored) enqueue<FEW, kMax, true>(a, sh, p, stream);
+    else enqueue<CHUNK, kMax, false>(a, sh, p, stream);
     set_launch_events(nullptr, nullptr);
     if (p.stored)
-        launch_kernel(fast ? lis_paged_sum_kernel<true> : lis_paged_sum_kernel<false>,
+        launch_kernel(mode_of(a) != kGeneral ? lis_paged_sum_kernel<true> : lis_paged_sum_kernel<false>,
                       dim3((uint32_t)(p.units * p.splits)), dim3(kBlock), 0, stream, a, sh);
-    else enqueue<RS, KS, NV, kSum, false>(a, sh, p, fast, stream);
+    else enqueue<CHUNK, kSum, false>(a, sh, p, stream);
     set_launch_events(nullptr, ev.stop);
-    if (p.stored) enqueue<1, KS, NV, kOut, true>(a, sh, p, fast, stream);
-    else enqueue<RS, KS, NV, kOut, false>(a, sh, p, fast, stream);
+    if (p.stored) enqueue<FEW, kOut, true>(a, sh, p, stream);
+    else enqueue<CHUNK, kOut, false>(a, sh, p, stream);
 }
 
 }  // namespace
 
 #if defined(FQ_PAGED_32)
-void launch_lis_paged_32(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<2, 1, 2>(a, sh, p, s); }
+void launch_lis_paged_32(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<2, 2, 2, 1, 2>, Config<1, 1, 4, 1, 2>>(a, sh, p, s); }
 #elif defined(FQ_PAGED_64)
-void launch_lis_paged_64(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<2, 1, 4>(a, sh, p, s); }
+void launch_lis_paged_64(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<2, 2, 2, 1, 4>, Config<1, 1, 4, 1, 4>>(a, sh, p, s); }
 #elif defined(FQ_PAGED_128)
-void launch_lis_paged_128(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<1, 2, 8>(a, sh, p, s); }
+void launch_lis_paged_128(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<1, 4, 1, 2, 8>, Config<1, 1, 2, 2, 8>>(a, sh, p, s); }
 #else
 void launch_lis_paged_32(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s);
 void launch_lis_paged_64(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s);
 void launch_lis_paged_128(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s);
 
-size_t lis_paged_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_t d,
+size_t lis_paged_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_t,
                            int64_t max_keys) {
-    return paged::plan(B, Hq, Hkv, L, d, max_keys).bytes();
+    return paged::plan(B, Hq, Hkv, L, max_keys).bytes();
 }
 
 hipError_t launch_lis_paged(const PagedArgs& a, hipStream_t stream) {
-    const Plan p = paged::plan(a.c.B, a.Hq, a.c.Hkv, a.L, a.c.d, (int64_t)a.c.max_pages << a.c.log2_page);
+    const Plan p = paged::plan(a.c.B, a.Hq, a.c.Hkv, a.L, (int64_t)a.c.max_pages << a.c.log2_page);
     Shape sh{};
     sh.splits = p.splits;
-    sh.row_groups = p.row_groups;
     sh.tiles = p.tiles;
     sh.rows = p.rows;
     sh.keys = p.keys;
     // the sums first: they need the largest alignment
-    sh.part_sum = static_cast<uint64_t*>(a.workspace);
-    sh.part_max = reinterpret_cast<int32_t*>(sh.part_sum + p.partials());
-    sh.logits = sh.part_max + (p.partials() + 3) / 4 * 4;
+    sh.row_sum = static_cast<uint64_t*>(a.workspace);
+    sh.row_max = reinterpret_cast<int32_t*>(sh.row_sum + p.all_rows());
+    sh.part_max = sh.row_max + p.all_rows();
+    sh.logits = sh.part_max + p.all_rows() * p.splits;
     while ((2u << sh.shift) * 2 <= a.k.d_ln2) ++sh.shift;       // 2^shift <= q_ln2 / 2
     const int cap = (a.k.n < a.k.top ? a.k.n : a.k.top) * (int)a.k.d_ln2;
     sh.buckets = ((cap - 1) >> sh.shift) + 2;

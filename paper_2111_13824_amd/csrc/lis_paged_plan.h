@@ -9,49 +9,43 @@
 namespace fqvit {
 namespace paged {
 
-constexpr int kWaves = 4;           // wavefronts of a workgroup
 constexpr int kTile = 64;           // keys a wavefront takes at a time
 
 struct Plan {
     int32_t stored;         // logits kept in the workspace between the passes (at most 16 rows)
     int32_t splits;         // parts of the keys, each a workgroup's; more than one: three launches
-    int32_t sets;           // sets of 16 rows a wavefront holds
-    int32_t row_groups;     // row groups of a workgroup; the other wavefronts share its keys
+    int32_t tile_rows;      // rows of a workgroup
     int32_t tiles;          // workgroups over the rows of a sequence and key head
     int32_t rows;           // rows of a sequence and key head
     int64_t units;          // sequences times key heads
     int64_t keys;           // keys a table names, up to a multiple of 64
 
-    int64_t tile_rows() const { return (int64_t)16 * sets * row_groups; }
-    // workspace: maxima [units, tiles, splits, tile_rows] int32, sums of 64 bits
-    // likewise, then the logits [units, rows, keys] int32
-    size_t partials() const { return splits > 1 ? (size_t)(units * tiles * splits * tile_rows()) : 0; }
+    // workspace of a divided call: of every row its sum (64 bits), its maximum and its
+    // parts' maxima (int32), then the logits [units, rows, keys] int32
+    size_t all_rows() const { return splits > 1 ? (size_t)(units * tiles * tile_rows) : 0; }
     size_t logits() const { return stored ? (size_t)(units * rows * keys) : 0; }
-    size_t bytes() const { return partials() * 12 + logits() * 4; }
+    size_t bytes() const { return all_rows() * (12 + 4 * splits) + logits() * 4; }
 };
 
 // What a kernel is told of it.
 struct Shape {
-    int32_t splits, row_groups, tiles, rows;
+    int32_t splits, tiles, rows;
     int64_t keys;               // row stride of the stored logits
-    int32_t* part_max;          // [units, tiles, splits, rows of a tile]
-    uint64_t* part_sum;
+    uint64_t* row_sum;          // [units, tiles, rows of a tile]
+    int32_t* row_max;           // likewise
+    int32_t* part_max;          // [units, tiles, rows of a tile, splits]
     int32_t* logits;            // [units, rows, keys]
     int32_t shift, buckets;     // of the thresholds' buckets
 };
 
-inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_t d, int64_t max_keys) {
+inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int64_t max_keys) {
     Plan p{};
     p.units = (int64_t)B * Hkv;
     p.rows = L * (Hq / Hkv);
     p.keys = (max_keys + kTile - 1) / kTile * kTile;
     p.splits = 1;
-    // two sets of rows share the operands of the keys; wide heads' results leave room for one
-    p.sets = p.rows > 16 && d <= 64 ? 2 : 1;
-    p.row_groups = 1;
-    if (p.rows > 64) p.row_groups = 2;
-    const auto count = [&] { return (int32_t)((p.rows + p.tile_rows() - 1) / p.tile_rows()); };
-    p.tiles = count();
+    p.tile_rows = p.rows <= 16 ? 16 : 64;
+    p.tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
     const int64_t groups = p.units * p.tiles;
     // parts of at least 512 keys until there are four workgroups a compute unit
     const int64_t most = p.keys / 512;
