@@ -28,13 +28,19 @@
 // Codes without I-Exp.  e(u), u = max - logit, does not increase with u (the host
 // checks the one place where rounding could make it, the end of an octave), so
 // code >= k, c_k e(u) <= 2 S (c_1 = 3, c_k = 3 2^(k-1) - 1), is u >= U_k for 2^b - 1
-// integers U_k of the row.  They are found exactly, once a row.  U_(k+1) - U_k is at
-// least q_ln2 for k >= 2 and above q_ln2 / 2 for k = 1, while U_k is not 0: buckets of
-// 2^shift <= q_ln2 / 2 values of u hold at most one threshold behind their first
-// value, and one word in LDS for each row and bucket, E = 2^24 (2^b - 1 - c) + th - 1
-// with c the code at the bucket's first u and th its threshold (or its end), gives
-// m = (E - u) >> 24.  A code costs five vector instructions and one LDS read where the
-// I-Exp and comparisons with S take about thirty.
+// integers U_k of the row.  They are found exactly, once a row.  U_1 exists, and
+// U_(k+1) - U_k is at least q_ln2 for k >= 2 where U_k is not 0 (e(u + q_ln2) = e(u) / 2,
+// c_(k+1) = 2 c_k + 1).  Buckets of 2^shift <= q_ln2 values of u from U_1 on hold
+// at most one threshold behind their first value (the first one U_2, the others none
+// closer), and one word of a bucket, E = 2^24 (2^b - 1 - c) + th - U_1 with c the code at its
+// first u and th the next threshold (or the bucket's end), gives m = (E + U_1 - 1 - u) >> 24.
+// U_1 - 1 - max is in the product's accumulators from the start; a code is a clamp, two
+// steps of an address, an LDS read and an addition, where the I-Exp and comparisons with S
+// are about thirty instructions.  Every lane has words of its own in its own LDS bank (one
+// table for a row's four lanes met five cycles of bank conflicts a read, and LDS bound
+// the pass).
+#include <algorithm>
+
 #include "cache_device.h"
 #include "fqvit_launch.h"
 #include "lis_device.h"
@@ -278,12 +284,14 @@ __device__ __forceinline__ int seen(int key0, int limit, int lane) {
 // Thresholds
 // ---------------------------------------------------------------------------
 
-// U_k: the least u in [0, n d] with c_k e(u) <= 2 S; n d + 1 where there is none.
+// U_k: the least u in [0, n d] with c_k e(u) <= 2 S; kNever where there is none.
 // With u = z d + rho, e = q_L(rho) 2^(n - z), q_L(rho) = (q_b - rho)^2 + q_c: the octave z is
 // the first whose last value satisfies it, n - z = floor(log2(2 S / (c_k q_L(d - 1)))),
 // settled by one comparison.  In it q_b - rho = floor(sqrt(X / c_k - q_c)), X =
 // floor(2 S / 2^(n - z)): from binary32 values that come within 2^-9 of it (q_L below
 // 2^24, c_k below 2^16: three roundings), so that the next integer is tried, exactly.
+constexpr int kNever = 1 << 20;         // above n d
+
 __device__ __forceinline__ int threshold(uint64_t S2, int k, const LisConsts& c) {
     const uint32_t ck = k == 1 ? 3u : (3u << (k - 1)) - 1u;
     const uint32_t wl = c.qb - c.d_ln2 + 1, last = wl * wl + c.qc, first = c.qb * c.qb + c.qc;
@@ -292,10 +300,9 @@ __device__ __forceinline__ int threshold(uint64_t S2, int k, const LisConsts& c)
     j = j >= 0 && (Q << j) > S2 ? j - 1 : j;
     const int z = c.n - min(max(j, 0), c.n);
     const uint64_t X = S2 >> (c.n - z);
-    const int none = c.n * (int)c.d_ln2 + 1;
     // the first value of the octave (of the last one, z = n, there is no other)
     if ((uint64_t)first * ck <= X) return z * (int)c.d_ln2;
-    if (z == c.n) return none;
+    if (z == c.n) return kNever;
     float w = (float)X * __builtin_amdgcn_rcpf((float)ck) - (float)c.qc;
     w = __builtin_amdgcn_sqrtf(fmaxf(w, 0.0f));
     uint32_t i = (uint32_t)(w + 0.5f);      // floor or one more
@@ -303,21 +310,24 @@ __device__ __forceinline__ int threshold(uint64_t S2, int k, const LisConsts& c)
     return z * (int)c.d_ln2 + (int)(c.qb - i);
 }
 
-// The words of a row's buckets, by the threads of a workgroup: bucket j >= 1 holds
-// u in ((j - 1) 2^shift, j 2^shift], bucket 0 u = 0.  They are stored backwards, so that
-// -u >> shift is the distance from the end; rows are 16 words apart.
+// Words of the buckets of rows whose U lies in LDS: bucket 0 holds u < U_1, bucket j >= 1
+// u in [U_1 + (j - 1) 2^shift, U_1 + j 2^shift).  They lie backwards, so that
+// (U_1 - 1 - u) >> shift counts from the end; a bucket's words are the 64 lanes', row
+// r's at r, r + 16, r + 32, r + 48.
 constexpr int kMaxTop = 15;
 
+// Those whose first u has code k.
 __device__ __forceinline__ void fill_buckets(const int* U, int k, int top, int shift, int buckets,
                                              uint32_t* words) {
-    // bucket j's code at its first u is the number of thresholds up to it: k for the
-    // buckets from the first whose first u reaches U_k to the one before U_(k+1)'s
-    const int u0 = k == 0 ? 0 : U[k - 1], u1 = k == top ? INT_MAX : U[k];
-    const auto from = [&](int u) { return u <= 0 ? 0 : (int)(((uint32_t)(u - 1) + (1u << shift) - 1) >> shift) + 1; };
-    const int end = u1 == INT_MAX ? buckets : min(from(u1), buckets);
-    for (int j = k == 0 ? 0 : from(u0); j < end; ++j) {
-        const int stop = (j << shift) + 1;          // behind the bucket's last u
-        words[16 * (buckets - 1 - j)] = ((uint32_t)(top - k) << 24) + (uint32_t)(min(u1, stop) - 1);
+    const int u1 = U[0], next = k == top ? INT_MAX : U[k];
+    // the first bucket whose first u reaches u
+    const auto from = [&](int u) { return u <= u1 ? 1 : ((u - u1 - 1) >> shift) + 2; };
+    const int end = k == top ? buckets : min(from(next), buckets);
+    for (int j = k == 0 ? 0 : from(U[k - 1]); j < (k == 0 ? 1 : end); ++j) {
+        const uint32_t e = ((uint32_t)(top - k) << 24) + (j == 0 ? 0u : (uint32_t)min(next - u1, j << shift));
+        uint32_t* w = words + 64 * (buckets - 1 - j);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) w[16 * g] = e;
     }
 }
 
@@ -376,6 +386,27 @@ __device__ __forceinline__ void digits(uint32_t m, uint32_t keep, uint32_t& hi, 
     const uint32_t up = __builtin_amdgcn_perm(0u, 0x0000FF00u, (m >> 3) & 0x01010101u);
     hi = v & up & keep;
     lo = v & ~up & keep;
+}
+
+// Sums over the 16 lanes of a block, of value e in lane e: at each step a lane hands half
+// of its values to another lane and takes that one's other half.
+__device__ __forceinline__ uint32_t sum16(const uint32_t (&v)[16], int lane) {
+    uint32_t a[8], b[4], c[2];
+    const bool b3 = lane & 8, b2 = lane & 4, b1 = lane & 2, b0 = lane & 1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)         // lane ^ 8
+        a[i] = (b3 ? v[8 + i] : v[i]) +
+               (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b3 ? v[i] : v[8 + i]), 0x128, 0xF, 0xF, true);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)         // lane ^ 7
+        b[i] = (b2 ? a[4 + i] : a[i]) +
+               (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b2 ? a[i] : a[4 + i]), 0x141, 0xF, 0xF, true);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)         // lane ^ 2
+        c[i] = (b1 ? b[2 + i] : b[i]) +
+               (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b1 ? b[i] : b[2 + i]), 0x4E, 0xF, 0xF, true);
+    return (b0 ? c[1] : c[0]) +         // lane ^ 1
+           (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b0 ? c[0] : c[1]), 0xB1, 0xF, 0xF, true);
 }
 
 // Maxima of the rows over all parts, a wavefront a row.
@@ -635,7 +666,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
         __syncthreads();
         for (int at = threadIdx.x; at < tile_rows * (a.k.top + 1); at += kBlock) {
             const int r = at % tile_rows, k = at / tile_rows;
-            fill_buckets(U[r], k, a.k.top, sh.shift, sh.buckets, dyn + (r >> 4) * (16 * sh.buckets) + (r & 15));
+            fill_buckets(U[r], k, a.k.top, sh.shift, sh.buckets, dyn + (r >> 4) * (64 * sh.buckets) + (r & 15));
         }
     } else {
 #pragma unroll
@@ -649,24 +680,24 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     // --- codes and product
     i32x4 hi[RS][NV] = {}, lo[RS][NV] = {}, ph[RS] = {}, pl[RS] = {};
     const i32x4 ones = splat(0x01010101);
-    const int cap = min(a.k.n, a.k.top) * (int)a.k.d_ln2;
+    const int cap = min(a.k.n, a.k.top) * (int)a.k.d_ln2 + 1;
     const auto product = [&](int key0, const i32x4 (&acc)[RS][4], const int8_t* values, bool edge) {
         i32x4 v[NV];
         st.read_v(values, v);
+        uint32_t got[16] = {};          // weights of the lane's keys over the sets
 #pragma unroll
         for (int s = 0; s < RS; ++s) {
             uint32_t m[4];
-            const uint32_t* end = dyn + (rg * RS + s) * (16 * sh.buckets) + 16 * (sh.buckets - 1) + (lane & 15);
+            const uint32_t* end = dyn + (rg * RS + s) * (64 * sh.buckets) + 64 * (sh.buckets - 1) + lane;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 uint32_t x[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (FAST) {
-                        // -u; a key that the row does not see may lie above its maximum
-                        int u;
+                        int u;          // U_1 - 1 - u
                         asm("v_med3_i32 %0, %1, %2, 0" : "=v"(u) : "v"(acc[s][t][i]), "s"(-cap));
-                        x[i] = end[(u >> sh.shift) * 16] + (uint32_t)u;
+                        x[i] = end[(u >> sh.shift) * 64] + (uint32_t)u;
                     } else {
                         uint32_t z;
                         const uint32_t qL = lis::iexp_qL(acc[s][t][i], mx[s], a.k, z);
@@ -700,29 +731,30 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
             // sums of the weights, for zp_v: cheaper than a branch on it
             ph[s] = mfma(ones, wh, ph[s]);
             pl[s] = mfma(ones, wl, pl[s]);
-            if (WEIGHT) {
-                const bool mine = row0 + 16 * s + (lane & 15) < rows;
+            if (WEIGHT && row0 + 16 * s + (lane & 15) < rows)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int8_t bh = (int8_t)((uint32_t)wh[e >> 2] >> (8 * (e & 3)));
-                    const int8_t bl = (int8_t)((uint32_t)wl[e >> 2] >> (8 * (e & 3)));
-                    int p = mine ? -(256 * bh + bl) : 0;
-#pragma unroll
-                    for (int o = 1; o < 16; o <<= 1) p += __shfl_xor(p, o);
-                    const int key = key0 + 16 * (lane >> 4) + e;
-                    if ((lane & 15) == e && key < len && p) {
-                        const int id = page_at(a.c.table, a.c.max_pages, a.c.pages, b, key >> a.c.log2_page);
-                        atomicAdd(reinterpret_cast<unsigned long long*>(a.c.weight) +
-                                      (((int64_t)id * a.c.Hkv + h) << a.c.log2_page) +
-                                      (key & ((1 << a.c.log2_page) - 1)),
-                                  (unsigned long long)p);
-                    }
-                }
+                for (int e = 0; e < 16; ++e)
+                    got[e] += (1u << ((m[e >> 2] >> (8 * (e & 3))) & 31u)) & ((uint32_t)keep[e >> 2] >> (8 * (e & 3)) & 1u ? ~0u : 0u);
+        }
+        if (WEIGHT) {
+            const uint32_t sum = sum16(got, lane);          // of key lane % 16 of the lane's block
+            const auto t = st.blocks(key0 - kg * kTile);
+            const int g = lane >> 4;
+            int64_t slot;
+            if (st.whole) {
+                slot = ((int64_t)((uint32_t)t.id[0] < (uint32_t)a.c.pages ? t.id[0] : 0) * a.c.Hkv + h) << a.c.log2_page;
+                slot += t.off[0] + 16 * g;
+            } else {
+                const int id = g & 2 ? (g & 1 ? t.id[3] : t.id[2]) : (g & 1 ? t.id[1] : t.id[0]);
+                const int off = g & 2 ? (g & 1 ? t.off[3] : t.off[2]) : (g & 1 ? t.off[1] : t.off[0]);
+                slot = ((int64_t)((uint32_t)id < (uint32_t)a.c.pages ? id : 0) * a.c.Hkv + h) << a.c.log2_page;
+                slot += off;
             }
+            if (sum) atomicAdd(reinterpret_cast<unsigned long long*>(a.c.weight) + slot + (lane & 15), (unsigned long long)sum);
         }
     };
 #pragma unroll
-    for (int s = 0; s < RS; ++s) add[s] = splat(FAST ? -mx[s] : 0);
+    for (int s = 0; s < RS; ++s) add[s] = splat(FAST ? U[rg * kRows + 16 * s + (lane & 15)][0] - 1 - mx[s] : 0);
     walk(add, std::true_type{}, product);
 
     // --- out: what the wavefronts of the other key groups hold comes to the first one's
@@ -732,7 +764,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
         for (int ct = 0; ct < NV; ++ct)
             lo[s][ct] = a.zp_v * (ph[s] * 256 + pl[s]) - (hi[s][ct] * 256 + lo[s][ct]);
     if (KG > 1) {
-        i32x4* held = reinterpret_cast<i32x4*>(dyn + (FAST ? tile_rows * sh.buckets : 0));
+        i32x4* held = reinterpret_cast<i32x4*>(dyn);        // the buckets are read
         if (kg > 0)
 #pragma unroll
             for (int s = 0; s < RS; ++s)
@@ -826,13 +858,13 @@ __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shap
 // ---------------------------------------------------------------------------
 
 // Whether the thresholds and the binary32 I-Exp hold for these constants: q_L below
-// 2^24 (which keeps d below 2^11), e(u) not increasing over an octave's end, buckets of
-// at least 8 values, the sums of a tile below 2^52, and -zp_q a byte.
+// 2^24 (which keeps d below 2^11), e(u) not increasing over an octave's end, the sums of
+// a tile below 2^52, and -zp_q a byte.
 Mode mode_of(const PagedArgs& a) {
     const LisConsts& k = a.k;
     const uint64_t first = (uint64_t)k.qb * k.qb + k.qc;
     const uint64_t w = k.qb - k.d_ln2 + 1, last = w * w + k.qc;
-    if (first >= (1u << 24) || 2 * last < first || k.d_ln2 < 16 || k.n > 23 || a.zp_q == -128) return kGeneral;
+    if (first >= (1u << 24) || 2 * last < first || k.n > 23 || a.zp_q == -128) return kGeneral;
     return k.s_pre ? kShifted : kPlain;
 }
 
@@ -840,9 +872,10 @@ template <class C, Pass PASS, bool STORED>
 void enqueue(const PagedArgs& a, const Shape& sh, const Plan& p, hipStream_t stream) {
     constexpr bool last = PASS == kAll || PASS == kOut;
     const Mode mode = mode_of(a);
-    const size_t lds = last ? 4 * (mode != kGeneral ? (size_t)C::rows * sh.buckets : 0) +
-                                  (size_t)(C::KG - 1) * C::RG * C::RS * C::NV * 1024
-                            : 0;
+    // the buckets, and after them what the key groups hold
+    const size_t buckets = mode != kGeneral ? (size_t)C::rows * sh.buckets * 16 : 0;
+    const size_t held = (size_t)(C::KG - 1) * C::RG * C::RS * C::NV * 1024;
+    const size_t lds = last ? std::max(buckets, held) : 0;
     const bool weight = last && a.c.weight;
     const auto kernel =
         mode == kPlain ? (weight ? lis_paged_kernel<C, PASS, STORED, kPlain, last>
@@ -906,8 +939,8 @@ hipError_t launch_lis_paged(const PagedArgs& a, hipStream_t stream) {
     sh.row_max = reinterpret_cast<int32_t*>(sh.row_sum + p.all_rows());
     sh.part_max = sh.row_max + p.all_rows();
     sh.logits = sh.part_max + p.all_rows() * p.splits;
-    while ((2u << sh.shift) * 2 <= a.k.d_ln2) ++sh.shift;       // 2^shift <= q_ln2 / 2
-    const int cap = (a.k.n < a.k.top ? a.k.n : a.k.top) * (int)a.k.d_ln2;
+    while ((2u << sh.shift) <= a.k.d_ln2) ++sh.shift;       // 2^shift <= q_ln2
+    const int cap = (a.k.n < a.k.top ? a.k.n : a.k.top) * (int)a.k.d_ln2 + 1;
     sh.buckets = ((cap - 1) >> sh.shift) + 2;
     if (a.c.d <= 32) launch_lis_paged_32(a, sh, p, stream);
     else if (a.c.d <= 64) launch_lis_paged_64(a, sh, p, stream);
