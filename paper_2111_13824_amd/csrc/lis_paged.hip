@@ -76,6 +76,67 @@ __device__ __forceinline__ int limit_of(const PagedArgs& a, int len, int fresh, 
     return a.causal ? min(max(len - fresh + rho / a.group + 1, 0), len) : len;
 }
 
+// What a workgroup works on.  Its unit, a sequence's key head, runs on one XCD, whose L2
+// then holds the keys that the unit's workgroups share; eight units in a row go to the
+// eight XCDs, and the longest sequences come first (of at most 64): the last workgroups to
+// start are short ones.  (Units in order, a run of them an XCD, left the XCD of the longest
+// sequence alone for the last third of the time.)
+struct Place {
+    int split, tile, b, h;
+    int64_t unit;
+};
+
+// PARTS: a call whose rows are few and whose keys are divided: a unit's parts, which add to
+// the same few results, stay on one or two XCDs.
+template <bool PARTS>
+__device__ __forceinline__ Place place_of(const PagedArgs& a, const Shape& sh, int lane) {
+    // fewer than 2^24 workgroups: 32-bit divisions
+    if (PARTS) {
+        const uint32_t block = (uint32_t)lis::xcd_remap(blockIdx.x, gridDim.x);
+        const uint32_t u = block / (uint32_t)sh.splits;
+        Place p;
+        p.split = (int)(block - u * (uint32_t)sh.splits);
+        p.tile = 0;
+        p.h = (int)(u / (uint32_t)a.c.B);
+        p.b = (int)(u - (uint32_t)p.h * (uint32_t)a.c.B);
+        p.unit = (int64_t)p.b * a.c.Hkv + p.h;
+        return p;
+    }
+    const uint32_t units = (uint32_t)a.c.B * (uint32_t)a.c.Hkv, per = (uint32_t)sh.tiles * (uint32_t)sh.splits;
+    const uint32_t even = units & ~7u, block = blockIdx.x;
+    uint32_t u, part;
+    if (block < even * per) {
+        const uint32_t i = block >> 3;
+        u = i / per;
+        part = i - u * per;
+        u = 8 * u + (block & 7);
+    } else {
+        const uint32_t i = block - even * per;
+        u = i / per;
+        part = i - u * per;
+        u += even;
+    }
+    Place p;
+    const uint32_t tile = part / (uint32_t)sh.splits;
+    p.split = (int)(part - tile * (uint32_t)sh.splits);
+    p.tile = sh.tiles - 1 - (int)tile;          // the rows that see most come first
+    int b = (int)(u / (uint32_t)a.c.Hkv);
+    p.h = (int)(u - (uint32_t)b * (uint32_t)a.c.Hkv);
+    if (a.c.B > 1 && a.c.B <= 64) {             // the sequence with b longer ones
+        const int mine = lane < a.c.B ? a.c.length[lane] : INT_MIN;
+        int rank = 0;
+        for (int i = 0; i < a.c.B; ++i) {
+            const int other = __builtin_amdgcn_readlane(mine, i);
+            rank += other > mine || (other == mine && i < lane) ? 1 : 0;
+        }
+        const uint64_t is = __ballot(lane < a.c.B && rank == b);
+        b = __ffsll((unsigned long long)is) - 1;
+    }
+    p.b = b;
+    p.unit = (int64_t)b * a.c.Hkv + p.h;
+    return p;
+}
+
 template <int KS>
 struct Operand {
     i32x4 w[KS];
@@ -109,7 +170,8 @@ struct Stage {
     const PagedArgs& a;
     int b, h, len, lane, wave;
     bool whole;                 // a page holds whole tiles
-    int64_t head, stride;       // bytes before the head in a page, bytes of a page
+    int64_t head;               // bytes before the head in a page
+    uint32_t stride;            // bytes of a page (at most 2^27)
 
     __device__ __forceinline__ Blocks blocks(int key0) const {
         typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
@@ -132,7 +194,7 @@ struct Stage {
     }
     // the head's first byte in a page; an id that is no page of the cache reads as page 0
     __device__ __forceinline__ int64_t base(int id) const {
-        return head + (int64_t)((uint32_t)id < (uint32_t)a.c.pages ? id : 0) * stride;
+        return head + (int64_t)((uint64_t)((uint32_t)id < (uint32_t)a.c.pages ? (uint32_t)id : 0u) * stride);
     }
 
     // A stage on its way.
@@ -429,32 +491,79 @@ struct Config {
     static constexpr int threads = 64 * RG * KG, rows = 16 * RS * RG;
 };
 
-template <class C, Pass PASS, bool STORED, Mode MODE, bool WEIGHT>
+// A sum over the lanes of a wavefront.
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// The I-Exp values of four stored logits of a row of maximum mx, those at `end` and behind left out.
+template <bool FAST>
+__device__ __forceinline__ uint64_t sum4(i32x4 v, int key0, int end, int mx, const PagedArgs& a) {
+    uint64_t sum = 0;
+    if (FAST) {
+        const int c = lis::screen_c(mx, a.k);
+        double s = __longlong_as_double((int64_t)(1023 + 52 - a.k.n) << 52);    // as in RowAdder
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t e = key0 + i < end ? lis::screen_iexp(v[i], c, a.k) : 0u;
+            s += (double)__uint_as_float(e);
+        }
+        sum = (uint64_t)__double_as_longlong(s) & ((1ull << 52) - 1);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t z;
+            const uint32_t qL = lis::iexp_qL(v[i], mx, a.k, z);
+            sum += key0 + i < end ? (uint64_t)qL << (a.k.n - (int)z) : 0;
+        }
+    }
+    return sum;
+}
+
+// f(row, key, end) for the rows and runs of 256 keys of [from, to), a wavefront a run, every lane
+// its four keys from `key` on; the row sees the keys before `end`.
+template <typename F>
+__device__ __forceinline__ void for_row_runs(const PagedArgs& a, int len, int fresh, int rows, int from, int to,
+                                             int lane, int wave, int waves, F&& f) {
+    const int runs = (to - from + 255) / 256;
+    for (int at = wave; at < rows * runs; at += waves) {
+        const int row = at / runs;
+        f(row, from + 256 * (at - row * runs) + 4 * lane, min(to, limit_of(a, len, fresh, row)));
+    }
+}
+
+// Logits between the passes: taken again, in the workspace, or in LDS.
+enum Keep { kNot, kWorkspace, kLds };
+
+template <class C, Pass PASS, Keep KEEP, Mode MODE, bool WEIGHT>
 __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, Shape sh) {
     constexpr int RS = C::RS, RG = C::RG, KG = C::KG, KS = C::KS, NV = C::NV;
     constexpr int kBlock = C::threads, tile_rows = C::rows, kRows = 16 * RS;
     constexpr bool FAST = MODE != kGeneral;
-    constexpr bool KEYS = !(STORED && PASS == kOut), VALUES = PASS == kAll || PASS == kOut;
+    constexpr bool VALUES = PASS == kAll || PASS == kOut;
+    // passes that take the logits from the keys, and the last one's way
+    constexpr bool STORED = KEEP != kNot, KEYS = !(STORED && PASS == kOut);
+    typedef std::integral_constant<bool, true> Yes;
+    typedef std::integral_constant<bool, false> No;
     typedef Stage<RG, KG, KS, NV> St;
-    // two stages
-    constexpr int kK = KEYS ? KG * St::kKeyBytes : 16, kV = VALUES ? KG * St::kValueBytes : 16;
-    __shared__ __attribute__((aligned(16))) int8_t stage_k[2][kK], stage_v[2][kV];
-    extern __shared__ uint32_t dyn[];               // buckets, then the workgroup's out
+    // two stages; with the logits in LDS a pass needs keys or values, not both
+    constexpr int kK = KG * St::kKeyBytes, kV = KG * St::kValueBytes;
+    constexpr int kStageK = !KEYS ? 16 : (KEEP == kLds ? (kK > kV ? kK : kV) : kK);
+    constexpr int kStageV = !VALUES || KEEP == kLds ? 16 : kV;
+    __shared__ __attribute__((aligned(16))) int8_t stage_k[2][kStageK], stage_v_[2][kStageV];
+    const auto stage_v = [&](int i) { return KEEP == kLds ? stage_k[i] : stage_v_[i]; };
+    extern __shared__ __attribute__((aligned(16))) uint32_t dyn[];     // buckets and logits, then the workgroup's out
     __shared__ int row_max[tile_rows];
     __shared__ unsigned long long row_sum[tile_rows];
     __shared__ int U[VALUES && FAST ? tile_rows : 1][kMaxTop];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rg = wave % RG, kg = wave / RG;
-    // fewer than 2^24 workgroups: 32-bit divisions
-    const uint32_t block = (uint32_t)lis::xcd_remap(blockIdx.x, gridDim.x);
-    const uint32_t wg = block / (uint32_t)sh.splits;
-    const int split = (int)(block - wg * (uint32_t)sh.splits);
-    const int64_t unit = wg / (uint32_t)sh.tiles;
-    // the rows that see most come first
-    const int tile = sh.tiles - 1 - (int)(wg - (uint32_t)unit * (uint32_t)sh.tiles);
-    // heads first: the workgroups of an XCD, which are neighbours, see several sequences
-    const int h = (int)((uint32_t)unit / (uint32_t)a.c.B), b = (int)unit - h * a.c.B;
+    const Place at = place_of<KEEP == kWorkspace>(a, sh, lane);
+    const int split = at.split, tile = at.tile, b = at.b, h = at.h;
+    const int64_t unit = at.unit;
     const int len = keys_of(a.c, b);
     const int fresh = a.n_new ? min(max(a.n_new[b], 0), a.L) : a.L;
     const int rows = fresh * a.group;
@@ -477,10 +586,13 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
 
     Queries<RS, KS> q;
     const int64_t head_bytes = (int64_t)a.c.d << a.c.log2_page;
-    const St st{a, b, h, len, lane, wave, a.c.log2_page >= 6, h * head_bytes, a.c.Hkv * head_bytes};
+    const St st{a, b, h, len, lane, wave, a.c.log2_page >= 6, h * head_bytes, (uint32_t)(a.c.Hkv * head_bytes)};
     if (KEYS) q.load(a, b, h, min(row0, rows - 1), rows, lane);
+    // the lane's row of the logits that are kept
+    int32_t* const lds_logits = reinterpret_cast<int32_t*>(dyn + (FAST ? tile_rows * 4 * sh.buckets : 0));
+    const int64_t lg_at = (int64_t)min(lane & 15, sh.rows - 1) * sh.keys + 16 * (lane >> 4);
     int32_t* lg = nullptr;
-    if (STORED) lg = sh.logits + (unit * sh.rows + min(lane & 15, sh.rows - 1)) * sh.keys + 16 * (lane >> 4);
+    if (KEEP == kWorkspace) lg = sh.logits + unit * sh.rows * sh.keys + lg_at;
 
     // body(key0, logits + add, values, edge) for each of the wavefront's tiles.  edge: a row
     // may not see all of it; the logits that it does not see are the lowest value.  What
@@ -489,46 +601,59 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     constexpr int step = KG * kTile;
     typename St::Loads r[2];
     typename St::Blocks next;
-    // the first two stages on their way
-    const auto prime = [&](auto with_values) {
-        constexpr bool V = decltype(with_values)::value;
+    // How many stages are on their way beside the two in LDS: values of wide heads, which a
+    // wavefront of few rows loads alone, leave registers for one.
+    const auto sets = [](auto values) { return decltype(values)::value && NV == 8 && RG == 1 ? 1 : 2; };
+    // the first stages on their way
+    const auto prime = [&](auto with_keys, auto with_values) {
+        constexpr bool K = decltype(with_keys)::value, V = decltype(with_values)::value;
         if (stages == 0) return;
         next = st.blocks(from);
-        st.template load<KEYS, V>(next, r[0]);
+        st.template load<K, V>(next, r[0]);
         next = st.blocks(from + step);
-        st.template load<KEYS, V>(next, r[1]);
-        next = st.blocks(from + 2 * step);
+        if (sets(with_values) == 2) {
+            st.template load<K, V>(next, r[1]);
+            next = st.blocks(from + 2 * step);
+        }
     };
-    const auto walk = [&](const i32x4 (&add)[RS], auto with_values, auto&& body) {
-        constexpr bool V = decltype(with_values)::value;
+    const auto walk = [&](const i32x4 (&add)[RS], auto with_keys, auto with_values, auto&& body) {
+        constexpr bool K = decltype(with_keys)::value, V = decltype(with_values)::value;
+        constexpr int kSets = V && NV == 8 && RG == 1 ? 1 : 2;
         if (stages == 0) return;
         const int own = from + kg * kTile;
-        st.template store<KEYS, V>(r[0], stage_k[0], stage_v[0]);
-        st.template load<KEYS, V>(next, r[0]);
-        next = st.blocks(from + 3 * step);
+        st.template store<K, V>(r[0], stage_k[0], stage_v(0));
+        st.template load<K, V>(next, r[0]);
+        next = st.blocks(from + (kSets + 1) * step);
         meet();
         const auto stored = [&](int key0, i32x4 (&acc)[RS][4]) {
+            const int k = min(key0, (int)sh.keys - kTile);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                acc[0][t] = *reinterpret_cast<const i32x4*>(lg + min(key0, (int)sh.keys - kTile) + 4 * t);
+                acc[0][t] = KEEP == kLds ? *reinterpret_cast<const i32x4*>(lds_logits + lg_at + k + 4 * t)
+                                         : *reinterpret_cast<const i32x4*>(lg + k + 4 * t);
         };
         i32x4 ahead[RS][4];
-        if (!KEYS) stored(own, ahead);
-        // stage n, of parity i: stage n + 1 goes into LDS, stage n + 3 is sent for
+        if (!K && KEEP == kWorkspace) stored(own, ahead);
+        // stage n, of parity i: stage n + 1 goes into LDS, the next that is not on its way is
+        // sent for
         const auto stage = [&](int n, auto i_, auto works) {
-            constexpr int i = decltype(i_)::value;
+            constexpr int i = decltype(i_)::value, o = kSets == 2 ? i ^ 1 : 0;
             const int key0 = own + n * step;
             i32x4 acc[RS][4];
-            st.template store<KEYS, V>(r[i ^ 1], stage_k[i ^ 1], stage_v[i ^ 1]);
-            if (!KEYS) {
+            st.template store<K, V>(r[o], stage_k[i ^ 1], stage_v(i ^ 1));
+            if (!K) {
+                if (KEEP == kLds) {
+                    stored(key0, acc);
+                } else {
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[0][t] = ahead[0][t];
-                stored(key0 + step, ahead);
+                    for (int t = 0; t < 4; ++t) acc[0][t] = ahead[0][t];
+                    stored(key0 + step, ahead);
+                }
             }
-            st.template load<KEYS, V>(next, r[i ^ 1]);
-            next = st.blocks(from + (n + 4) * step);
+            st.template load<K, V>(next, r[o]);
+            next = st.blocks(from + (n + kSets + 2) * step);
             if (decltype(works)::value) {
-                if (KEYS) {
+                if (K) {
                     Operand<KS> k[4];
                     st.read_k(stage_k[i], k);
                     q.template logits<FAST>(k, add, acc);
@@ -547,7 +672,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
                             for (int x = 0; x < 4; ++x) acc[s][t][x] = 4 * t + x < n_seen ? acc[s][t][x] : INT_MIN;
                     }
                 }
-                body(key0, acc, stage_v[i], edge);
+                body(key0, acc, stage_v(i), edge);
             }
             meet();
         };
@@ -566,7 +691,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     // the workgroup's rows in the workspace
     const int64_t row_at = (unit * sh.tiles + tile) * tile_rows;
     i32x4 add[RS];
-    prime(std::integral_constant<bool, PASS == kOut>{});
+    prime(std::integral_constant<bool, KEYS>{}, std::integral_constant<bool, PASS == kOut>{});
 
     // --- maximum
     for (int i = threadIdx.x; i < tile_rows; i += kBlock) {
@@ -581,14 +706,14 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
             mx[s] = INT_MIN;
             add[s] = splat(0);
         }
-        walk(add, std::false_type{}, [&](int key0, const i32x4 (&acc)[RS][4], const int8_t*, bool) {
+        walk(add, Yes{}, No{}, [&](int key0, const i32x4 (&acc)[RS][4], const int8_t*, bool) {
 #pragma unroll
             for (int s = 0; s < RS; ++s)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     mx[s] = max(max(max(mx[s], acc[s][t][0]), acc[s][t][1]), max(acc[s][t][2], acc[s][t][3]));
                     if (STORED && (lane & 15) < sh.rows && key0 < to)
-                        *reinterpret_cast<i32x4*>(lg + key0 + 4 * t) = acc[s][t];
+                        *reinterpret_cast<i32x4*>((KEEP == kLds ? lds_logits + lg_at : lg) + key0 + 4 * t) = acc[s][t];
                 }
         });
 #pragma unroll
@@ -631,11 +756,22 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
 #pragma unroll
     for (int s = 0; s < RS; ++s) mx[s] = row_max[rg * kRows + 16 * s + (lane & 15)];
     if (PASS == kAll || PASS == kSum) {
-        if (PASS == kAll) prime(std::false_type{});
+        if (KEEP == kLds) {
+            prime(No{}, Yes{});
+            for_row_runs(a, len, fresh, rows, from, until, lane, wave, KG * RG, [&](int row, int key0, int end) {
+                uint64_t v = 0;
+                if (key0 < end)
+                    v = sum4<FAST>(*reinterpret_cast<const i32x4*>(lds_logits + row * (int)sh.keys + key0), key0, end,
+                                   row_max[row], a);
+                v = wave_sum(v);
+                if (lane == 0) atomicAdd(&row_sum[row], (unsigned long long)v);
+            });
+        } else {
+        if (PASS == kAll) prime(Yes{}, No{});
         RowAdder<MODE> sum[RS];
 #pragma unroll
         for (int s = 0; s < RS; ++s) add[s] = splat(FAST ? -lis::screen_c(mx[s], a.k) : 0);
-        walk(add, std::false_type{}, [&](int key0, const i32x4 (&acc)[RS][4], const int8_t*, bool edge) {
+        walk(add, Yes{}, No{}, [&](int key0, const i32x4 (&acc)[RS][4], const int8_t*, bool edge) {
 #pragma unroll
             for (int s = 0; s < RS; ++s) sum[s].add(acc[s], mx[s], a);
             if (edge)
@@ -647,6 +783,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
             const uint64_t v = lis::row4_sum(sum[s].sum);
             if (lane < 16) atomicAdd(&row_sum[rg * kRows + 16 * s + lane], (unsigned long long)v);
         }
+        }
         __syncthreads();
         if (PASS == kSum) {
             for (int i = threadIdx.x; i < tile_rows; i += kBlock)
@@ -656,7 +793,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     }
 
     // --- thresholds
-    if (PASS == kAll) prime(std::true_type{});
+    if (PASS == kAll && KEEP == kNot) prime(Yes{}, Yes{});
     lis::RowSum rs[RS];
     if (FAST) {
         for (int at = threadIdx.x; at < tile_rows * a.k.top; at += kBlock) {
@@ -755,7 +892,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     };
 #pragma unroll
     for (int s = 0; s < RS; ++s) add[s] = splat(FAST ? U[rg * kRows + 16 * s + (lane & 15)][0] - 1 - mx[s] : 0);
-    walk(add, std::true_type{}, product);
+    walk(add, std::integral_constant<bool, !STORED>{}, Yes{}, product);
 
     // --- out: what the wavefronts of the other key groups hold comes to the first one's
 #pragma unroll
@@ -805,10 +942,9 @@ __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shap
     __shared__ int row_max[16];
     __shared__ unsigned long long row_sum[16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t block = (uint32_t)lis::xcd_remap(blockIdx.x, gridDim.x);
-    const int64_t unit = block / (uint32_t)sh.splits;
-    const int split = (int)(block - (uint32_t)unit * (uint32_t)sh.splits);
-    const int b = (int)((uint32_t)unit % (uint32_t)a.c.B);
+    const Place place = place_of<true>(a, sh, lane);
+    const int split = place.split, b = place.b;
+    const int64_t unit = place.unit;
     const int len = keys_of(a.c, b);
     const int fresh = a.n_new ? min(max(a.n_new[b], 0), a.L) : a.L;
     const int rows = fresh * a.group;
@@ -821,33 +957,14 @@ __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shap
     parts_max(sh, row_at, rows, lane, wave, kBlock / 64, row_max);
     __syncthreads();
     if (split == 0 && threadIdx.x < rows) sh.row_max[row_at + threadIdx.x] = row_max[threadIdx.x];
-    const int runs = (to - from + 255) / 256;
-    for (int at = wave; at < rows * runs; at += kBlock / 64) {
-        const int r = at / runs, key0 = from + 256 * (at - r * runs) + 4 * lane;
-        const int end = min(to, limit_of(a, len, fresh, r));
-        uint64_t sum = 0;
-        if (key0 < end) {
-            const i32x4 v = *reinterpret_cast<const i32x4*>(sh.logits + (unit * sh.rows + r) * sh.keys + key0);
-            const int c = lis::screen_c(row_max[r], a.k);
-            const double unit_n = __longlong_as_double((int64_t)(1023 + 52 - a.k.n) << 52);
-            double s = unit_n;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (FAST) {
-                    const uint32_t e = key0 + i < end ? lis::screen_iexp(v[i], c, a.k) : 0u;
-                    s += (double)__uint_as_float(e);
-                } else {
-                    uint32_t z;
-                    const uint32_t qL = lis::iexp_qL(v[i], row_max[r], a.k, z);
-                    sum += key0 + i < end ? (uint64_t)qL << (a.k.n - (int)z) : 0;
-                }
-            }
-            if (FAST) sum = (uint64_t)__double_as_longlong(s) & ((1ull << 52) - 1);
-        }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0) atomicAdd(&row_sum[r], (unsigned long long)sum);
-    }
+    const int32_t* lg = sh.logits + unit * sh.rows * sh.keys;
+    for_row_runs(a, len, fresh, rows, from, to, lane, wave, kBlock / 64, [&](int row, int key0, int end) {
+        uint64_t v = 0;
+        if (key0 < end)
+            v = sum4<FAST>(*reinterpret_cast<const i32x4*>(lg + row * sh.keys + key0), key0, end, row_max[row], a);
+        v = wave_sum(v);
+        if (lane == 0) atomicAdd(&row_sum[row], (unsigned long long)v);
+    });
     __syncthreads();
     if (threadIdx.x < rows)
         atomicAdd(reinterpret_cast<unsigned long long*>(sh.row_sum) + row_at + threadIdx.x, row_sum[threadIdx.x]);
@@ -868,55 +985,54 @@ Mode mode_of(const PagedArgs& a) {
     return k.s_pre ? kShifted : kPlain;
 }
 
-template <class C, Pass PASS, bool STORED>
+template <class C, Pass PASS, Keep KEEP>
 void enqueue(const PagedArgs& a, const Shape& sh, const Plan& p, hipStream_t stream) {
     constexpr bool last = PASS == kAll || PASS == kOut;
     const Mode mode = mode_of(a);
     // the buckets, and after them what the key groups hold
     const size_t buckets = mode != kGeneral ? (size_t)C::rows * sh.buckets * 16 : 0;
     const size_t held = (size_t)(C::KG - 1) * C::RG * C::RS * C::NV * 1024;
-    const size_t lds = last ? std::max(buckets, held) : 0;
+    const size_t logits = KEEP == kLds ? (size_t)(p.rows * p.keys) * 4 : 0;
+    const size_t lds = last ? std::max(buckets + logits, held) : 0;
     const bool weight = last && a.c.weight;
     const auto kernel =
-        mode == kPlain ? (weight ? lis_paged_kernel<C, PASS, STORED, kPlain, last>
-                                 : lis_paged_kernel<C, PASS, STORED, kPlain, false>)
-        : mode == kShifted ? (weight ? lis_paged_kernel<C, PASS, STORED, kShifted, last>
-                                     : lis_paged_kernel<C, PASS, STORED, kShifted, false>)
-                           : (weight ? lis_paged_kernel<C, PASS, STORED, kGeneral, last>
-                                     : lis_paged_kernel<C, PASS, STORED, kGeneral, false>);
+        mode == kPlain ? (weight ? lis_paged_kernel<C, PASS, KEEP, kPlain, last>
+                                 : lis_paged_kernel<C, PASS, KEEP, kPlain, false>)
+        : mode == kShifted ? (weight ? lis_paged_kernel<C, PASS, KEEP, kShifted, last>
+                                     : lis_paged_kernel<C, PASS, KEEP, kShifted, false>)
+                           : (weight ? lis_paged_kernel<C, PASS, KEEP, kGeneral, last>
+                                     : lis_paged_kernel<C, PASS, KEEP, kGeneral, false>);
     launch_kernel(kernel, dim3((uint32_t)(p.units * p.tiles * p.splits)), dim3(C::threads), lds, stream, a, sh);
 }
 
 // CHUNK: more than 16 rows; FEW: up to 16.
 template <class CHUNK, class FEW>
 void launch(const PagedArgs& a, const Shape& sh, const Plan& p, hipStream_t stream) {
-    if (p.splits == 1) {
-        if (p.rows <= 16) enqueue<FEW, kAll, false>(a, sh, p, stream);
-        else enqueue<CHUNK, kAll, false>(a, sh, p, stream);
-        return;
-    }
+    if (p.way == paged::kOneFew) return enqueue<FEW, kAll, kLds>(a, sh, p, stream);
+    if (p.way == paged::kOne) return enqueue<CHUNK, kAll, kNot>(a, sh, p, stream);
+    const bool few = p.way == paged::kPartsFew;
     const LaunchEvents ev = launch_events();
     set_launch_events(ev.start, nullptr);
-    if (p.stored) enqueue<FEW, kMax, true>(a, sh, p, stream);
-    else enqueue<CHUNK, kMax, false>(a, sh, p, stream);
+    if (few) enqueue<FEW, kMax, kWorkspace>(a, sh, p, stream);
+    else enqueue<CHUNK, kMax, kNot>(a, sh, p, stream);
     set_launch_events(nullptr, nullptr);
-    if (p.stored)
+    if (few)
         launch_kernel(mode_of(a) != kGeneral ? lis_paged_sum_kernel<true> : lis_paged_sum_kernel<false>,
                       dim3((uint32_t)(p.units * p.splits)), dim3(kBlock), 0, stream, a, sh);
-    else enqueue<CHUNK, kSum, false>(a, sh, p, stream);
+    else enqueue<CHUNK, kSum, kNot>(a, sh, p, stream);
     set_launch_events(nullptr, ev.stop);
-    if (p.stored) enqueue<FEW, kOut, true>(a, sh, p, stream);
-    else enqueue<CHUNK, kOut, false>(a, sh, p, stream);
+    if (few) enqueue<FEW, kOut, kWorkspace>(a, sh, p, stream);
+    else enqueue<CHUNK, kOut, kNot>(a, sh, p, stream);
 }
 
 }  // namespace
 
 #if defined(FQ_PAGED_32)
-void launch_lis_paged_32(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<2, 2, 2, 1, 2>, Config<1, 1, 4, 1, 2>>(a, sh, p, s); }
+void launch_lis_paged_32(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<1, 4, 1, 1, 2>, Config<1, 1, 8, 1, 2>>(a, sh, p, s); }
 #elif defined(FQ_PAGED_64)
-void launch_lis_paged_64(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<2, 2, 2, 1, 4>, Config<1, 1, 4, 1, 4>>(a, sh, p, s); }
+void launch_lis_paged_64(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<1, 4, 1, 1, 4>, Config<1, 1, 8, 1, 4>>(a, sh, p, s); }
 #elif defined(FQ_PAGED_128)
-void launch_lis_paged_128(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<1, 4, 1, 2, 8>, Config<1, 1, 2, 2, 8>>(a, sh, p, s); }
+void launch_lis_paged_128(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<1, 4, 1, 2, 8>, Config<1, 1, 4, 2, 8>>(a, sh, p, s); }
 #else
 void launch_lis_paged_32(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s);
 void launch_lis_paged_64(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s);

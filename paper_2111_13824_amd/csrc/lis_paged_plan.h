@@ -11,9 +11,17 @@ namespace paged {
 
 constexpr int kTile = 64;           // keys a wavefront takes at a time
 
+// One launch whose passes take the logits again; one for at most 16 rows, which keeps
+// them in LDS; three launches over parts of the keys, without and (at most 16 rows) with
+// the logits in the workspace.
+enum Way { kOne, kOneFew, kParts, kPartsFew };
+
+// Logits of a workgroup that LDS holds beside two stages, the buckets and the rest.
+constexpr int64_t kLdsLogits = 16384;
+
 struct Plan {
-    int32_t stored;         // logits kept in the workspace between the passes (at most 16 rows)
-    int32_t splits;         // parts of the keys, each a workgroup's; more than one: three launches
+    Way way;
+    int32_t splits;         // parts of the keys, each a workgroup's
     int32_t tile_rows;      // rows of a workgroup
     int32_t tiles;          // workgroups over the rows of a sequence and key head
     int32_t rows;           // rows of a sequence and key head
@@ -22,8 +30,8 @@ struct Plan {
 
     // workspace of a divided call: of every row its sum (64 bits), its maximum and its
     // parts' maxima (int32), then the logits [units, rows, keys] int32
-    size_t all_rows() const { return splits > 1 ? (size_t)(units * tiles * tile_rows) : 0; }
-    size_t logits() const { return stored ? (size_t)(units * rows * keys) : 0; }
+    size_t all_rows() const { return way >= kParts ? (size_t)(units * tiles * tile_rows) : 0; }
+    size_t logits() const { return way == kPartsFew ? (size_t)(units * rows * keys) : 0; }
     size_t bytes() const { return all_rows() * (12 + 4 * splits) + logits() * 4; }
 };
 
@@ -47,15 +55,16 @@ inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int64_t max_keys
     p.tile_rows = p.rows <= 16 ? 16 : 64;
     p.tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
     const int64_t groups = p.units * p.tiles;
-    // parts of at least 512 keys until there are four workgroups a compute unit
-    const int64_t most = p.keys / 512;
-    int64_t want = 1024 / (groups > 0 ? groups : 1);
-    if (want > most) want = most;
-    if (want > 256) want = 256;
-    if (p.keys > 1024 && want > 1) {
-        p.splits = (int32_t)want;
-        p.stored = p.rows <= 16;
+    if (p.rows <= 16 && p.rows * p.keys <= kLdsLogits) {
+        p.way = kOneFew;
+        return p;
     }
+    // parts of at least 1024 keys until there are two workgroups a compute unit
+    int64_t want = 512 / (groups > 0 ? groups : 1);
+    if (want > p.keys / 1024) want = p.keys / 1024;
+    if (want > 256) want = 256;
+    if (want > 1) p.splits = (int32_t)want;
+    p.way = p.rows <= 16 ? kPartsFew : (p.splits > 1 ? kParts : kOne);
     return p;
 }
 
