@@ -156,27 +156,32 @@ hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream) {
 namespace {
 
 constexpr int kSelect = 1024;
-
-__device__ __forceinline__ int64_t weight_at(const CacheView& c, int b, int h, int place) {
-    const int id = page_at(c.table, c.max_pages, c.pages, b, place >> c.log2_page);
-    return c.weight[(((int64_t)id * c.Hkv + h) << c.log2_page) + (place & ((1 << c.log2_page) - 1))];
-}
+constexpr int kSelectWaves = kSelect / 64;
 
 // Order of signed weights as unsigned numbers.
 __device__ __forceinline__ uint64_t rank_of(int64_t w) { return (uint64_t)w ^ (1ull << 63); }
 
-// The places that stay, one workgroup for each sequence and head.  The m-th heaviest
-// of the old keys is found digit by digit (8 bits, a histogram in LDS) from the first
-// bit in which the weights differ; then one pass in order takes what is heavier and as
-// many of its equals, from the lowest place on, as are missing.
+__device__ __forceinline__ const int64_t* weight_slot(const CacheView& c, int b, int h, int place) {
+    const int id = page_at(c.table, c.max_pages, c.pages, b, place >> c.log2_page);
+    return c.weight + (((int64_t)id * c.Hkv + h) << c.log2_page) + (place & ((1 << c.log2_page) - 1));
+}
+
+// The places that stay, one workgroup for each sequence and head.  A thread holds ITEMS
+// neighbouring weights (ITEMS 0: reads runs of 8 again in each pass).  The m-th heaviest of the
+// old keys is found digit by digit (8 bits, a histogram in LDS, whose sums from the top
+// one wavefront takes) from the first bit in which the weights differ; then one scan
+// over the threads places what is heavier and as many of its equals, from the lowest
+// place on, as are missing.  (A histogram that one thread walks takes 10 us a digit.)
+template <int ITEMS>
 __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
     __shared__ uint32_t hist[256];
-    __shared__ uint64_t wide[kSelect / 64];
-    __shared__ uint32_t part[2][kSelect / 64];
+    __shared__ uint64_t wide[kSelectWaves];
+    __shared__ uint32_t part[2][kSelectWaves];
     __shared__ uint64_t bound;
     __shared__ int missing;
+    constexpr int kHeld = ITEMS ? ITEMS : 8;
     const CacheView& c = a.c;
-    const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x;
+    const int b = blockIdx.y, h = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = keys_of(c, b);
     int32_t* kept = a.kept + ((int64_t)b * c.Hkv + h) * a.keep;
     if (n <= a.keep) {
@@ -187,15 +192,43 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
     for (int j = tid; j < a.recent; j += kSelect) kept[m + j] = old + j;
     if (m == 0) return;
 
-    const uint64_t w0 = rank_of(weight_at(c, b, h, 0));
+    // f(first place, weights) for the thread's runs; the places at `old` and behind do not count
+    uint64_t held[kHeld];
+    const auto fetch = [&](int place, uint64_t* w) {
+        if (place >= old) return;
+        const int64_t* p = weight_slot(c, b, h, place);         // 8 places lie in one page
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = rank_of(p[e]);
+    };
+    if (ITEMS)
+#pragma unroll
+        for (int g = 0; g < kHeld; g += 8) fetch(tid * ITEMS + g, held + g);
+    const int runs = (old + 8 * kSelect - 1) / (8 * kSelect);
+    const auto each = [&](auto&& f) {
+        if (ITEMS) {
+#pragma unroll
+            for (int e = 0; e < kHeld; ++e)
+                if (tid * ITEMS + e < old) f(held[e]);
+        } else {
+            for (int r = 0; r < runs; ++r) {
+                const int place = 8 * (r * kSelect + tid);
+                fetch(place, held);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (place + e < old) f(held[e]);
+            }
+        }
+    };
+
+    const uint64_t w0 = rank_of(*weight_slot(c, b, h, 0));
     uint64_t diff = 0;
-    for (int j = tid; j < old; j += kSelect) diff |= rank_of(weight_at(c, b, h, j)) ^ w0;
+    each([&](uint64_t w) { diff |= w ^ w0; });
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) diff |= __shfl_xor(diff, o);
-    if ((tid & 63) == 0) wide[tid >> 6] = diff;
+    if (lane == 0) wide[wave] = diff;
     __syncthreads();
     diff = 0;
-    for (int i = 0; i < kSelect / 64; ++i) diff |= wide[i];
+    for (int i = 0; i < kSelectWaves; ++i) diff |= wide[i];
     // bits [0, top) differ; the others are w0's
     const int top = diff ? 64 - __clzll((long long)diff) : 0;
     uint64_t prefix = top < 64 ? w0 >> top << top : 0;
@@ -203,18 +236,31 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
     for (int hi = top; hi > 0;) {
         const int lo = max(hi - 8, 0);
         const uint32_t mask = (1u << (hi - lo)) - 1;
-        for (int i = tid; i < 256; i += kSelect) hist[i] = 0;
+        if (tid < 256) hist[tid] = 0;
         __syncthreads();
-        for (int j = tid; j < old; j += kSelect) {
-            const uint64_t w = rank_of(weight_at(c, b, h, j));
+        each([&](uint64_t w) {
             if (hi == 64 || (w >> hi) == (prefix >> hi)) atomicAdd(&hist[(uint32_t)(w >> lo) & mask], 1u);
-        }
+        });
         __syncthreads();
-        if (tid == 0) {         // the digit of the need-th heaviest
-            int left = need, digit = (int)mask;
-            while (digit > 0 && left > (int)hist[digit]) left -= (int)hist[digit--];
-            bound = prefix | ((uint64_t)digit << lo);
-            missing = left;
+        if (wave == 0) {        // the digit of the need-th heaviest: lane l holds the bins 255 - 4 l and below
+            uint32_t v[4], sum = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += v[e] = hist[255 - 4 * lane - e];
+            uint32_t before = sum;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const uint32_t x = __shfl_up(before, o);
+                before += lane >= o ? x : 0;
+            }
+            before -= sum;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if ((uint32_t)need > before && (uint32_t)need <= before + v[e]) {
+                    bound = prefix | ((uint64_t)(255 - 4 * lane - e) << lo);
+                    missing = need - (int)before;
+                }
+                before += v[e];
+            }
         }
         __syncthreads();
         prefix = bound;
@@ -223,31 +269,47 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
     }
     // heavier than `prefix`: m - need of them; of its equals the first `need`
     int done_heavy = 0, done_equal = 0;
-    for (int j0 = 0; j0 < old; j0 += kSelect) {
-        const int j = j0 + tid;
-        const uint64_t w = j < old ? rank_of(weight_at(c, b, h, j)) : 0;
-        const bool heavy = j < old && w > prefix, equal = j < old && w == prefix;
-        const uint64_t hm = __ballot(heavy), em = __ballot(equal);
-        const uint64_t below = (1ull << (tid & 63)) - 1;
-        __syncthreads();
-        if ((tid & 63) == 0) {
-            part[0][tid >> 6] = (uint32_t)__popcll(hm);
-            part[1][tid >> 6] = (uint32_t)__popcll(em);
-        }
-        __syncthreads();
-        int heavies = done_heavy, equals = done_equal;
-        for (int i = 0; i < kSelect / 64; ++i) {
-            const int nh = (int)part[0][i], ne = (int)part[1][i];
-            if (i < tid >> 6) {
-                heavies += nh;
-                equals += ne;
+    for (int r = 0; r < (ITEMS ? 1 : runs); ++r) {
+        const int place = ITEMS ? tid * ITEMS : 8 * (r * kSelect + tid);
+        if (!ITEMS) fetch(place, held);
+        uint32_t nh = 0, ne = 0;
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e)
+            if (place + e < old) {
+                nh += held[e] > prefix;
+                ne += held[e] == prefix;
             }
-            done_heavy += nh;
-            done_equal += ne;
+        uint32_t sh = nh, se = ne;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t xh = __shfl_up(sh, o), xe = __shfl_up(se, o);
+            sh += lane >= o ? xh : 0;
+            se += lane >= o ? xe : 0;
         }
-        heavies += __popcll(hm & below);
-        equals += __popcll(em & below);
-        if (heavy || (equal && equals < need)) kept[heavies + min(equals, need)] = j;
+        __syncthreads();
+        if (lane == 63) {
+            part[0][wave] = sh;
+            part[1][wave] = se;
+        }
+        __syncthreads();
+        int heavies = done_heavy + (int)(sh - nh), equals = done_equal + (int)(se - ne);
+        for (int i = 0; i < kSelectWaves; ++i) {
+            if (i < wave) {
+                heavies += (int)part[0][i];
+                equals += (int)part[1][i];
+            }
+            done_heavy += (int)part[0][i];
+            done_equal += (int)part[1][i];
+        }
+#pragma unroll
+        for (int e = 0; e < kHeld; ++e)
+            if (place + e < old) {
+                if (held[e] > prefix) kept[heavies++ + min(equals, need)] = place + e;
+                else if (held[e] == prefix) {
+                    if (equals < need) kept[heavies + equals] = place + e;
+                    ++equals;
+                }
+            }
     }
 }
 
@@ -265,78 +327,71 @@ __global__ __launch_bounds__(kBlock) void evict_move_kernel(EvictArgs a) {
     const CacheView& c = a.c;
     const int parts = 2 + (c.d >> 4);
     const int part = blockIdx.x % parts, h = blockIdx.x / parts, b = blockIdx.y;
-    const int n = keys_of(c, b);
-    const bool in_place = a.table_out == c.table;
-    const int stay = min(n, a.keep);
-    // a sequence within its budget stays where it is
-    const bool move = !(in_place && n <= a.keep);
     const int32_t* kept = a.kept + ((int64_t)b * c.Hkv + h) * a.keep;
-    const int page = 1 << c.log2_page, d = c.d;
+    const int page = 1 << c.log2_page, d = c.d, most = (c.max_pages << c.log2_page) - 1;
+    // the length is read by nothing else here: it may be written in place
+    if (part == 0 && h == 0 && blockIdx.z == 0 && threadIdx.x == 0) a.length_out[b] = min(keys_of(c, b), a.keep);
+    // place that j comes from; behind the last that stays: none
+    const auto from = [&](int j) { return j < a.keep ? min(kept[j], most) : -1; };
     // the page that place j goes to; none: nothing is written
     const auto target = [&](int j) {
         const int id = a.table_out[(int64_t)b * a.max_out + (j >> c.log2_page)];
         return (uint32_t)id < (uint32_t)c.pages ? id : -1;
     };
     const auto source = [&](int j) { return page_at(c.table, c.max_pages, c.pages, b, j >> c.log2_page); };
-    if (move && part == 0) {
+    if (part == 0) {
         const int chunks = d >> 4, tile = kBlock * kMoveUnits / chunks;       // keys
-        for (int j0 = blockIdx.z * tile; j0 < stay; j0 += gridDim.z * tile) {
+        for (int j0 = blockIdx.z * tile; j0 < a.keep; j0 += gridDim.z * tile) {
             u32x4 w[kMoveUnits];
+            bool live[kMoveUnits];
 #pragma unroll
             for (int u = 0; u < kMoveUnits; ++u) {
                 const int at = threadIdx.x + kBlock * u, j = j0 + at / chunks, ch = at % chunks;
-                if (at >= tile * chunks || j >= stay) continue;
-                const int s = min(max(kept[j], 0), n - 1);
-                w[u] = *reinterpret_cast<const u32x4*>(c.k + head_base(c, source(s), h) +
-                                                       (int64_t)(s & (page - 1)) * d + 16 * ch);
+                const int s = at < tile * chunks ? from(j) : -1;
+                live[u] = s >= 0;
+                if (live[u])
+                    w[u] = *reinterpret_cast<const u32x4*>(c.k + head_base(c, source(s), h) +
+                                                           (int64_t)(s & (page - 1)) * d + 16 * ch);
             }
             __syncthreads();
 #pragma unroll
             for (int u = 0; u < kMoveUnits; ++u) {
                 const int at = threadIdx.x + kBlock * u, j = j0 + at / chunks, ch = at % chunks;
-                if (at >= tile * chunks || j >= stay) continue;
-                const int to = target(j);
+                const int to = live[u] ? target(j) : -1;
                 if (to >= 0)
                     *reinterpret_cast<u32x4*>(c.k + head_base(c, to, h) + (int64_t)(j & (page - 1)) * d +
                                               16 * ch) = w[u];
             }
         }
-    } else if (move && part < parts - 1) {
+    } else if (part < parts - 1) {
         // 256 keys of 16 channels a tile: a lane holds 16 channels of one key
         const int c0 = 16 * (part - 1);
-        for (int j0 = blockIdx.z * kBlock; j0 < stay; j0 += gridDim.z * kBlock) {
-            const int j = j0 + threadIdx.x;
+        for (int j0 = blockIdx.z * kBlock; j0 < a.keep; j0 += gridDim.z * kBlock) {
+            const int j = j0 + threadIdx.x, s = from(j);
             int8_t w[kMoveBytes];
-            if (j < stay) {
-                const int s = min(max(kept[j], 0), n - 1);
+            if (s >= 0) {
                 const int8_t* src = c.v + head_base(c, source(s), h) + (int64_t)c0 * page + (s & (page - 1));
 #pragma unroll
                 for (int e = 0; e < kMoveBytes; ++e) w[e] = src[(int64_t)e * page];
             }
             __syncthreads();
-            const int to = j < stay ? target(j) : -1;
+            const int to = s >= 0 ? target(j) : -1;
             if (to >= 0) {
                 int8_t* dst = c.v + head_base(c, to, h) + (int64_t)c0 * page + (j & (page - 1));
 #pragma unroll
                 for (int e = 0; e < kMoveBytes; ++e) dst[(int64_t)e * page] = w[e];
             }
         }
-    } else if (part == parts - 1) {
-        for (int j0 = blockIdx.z * kBlock; move && j0 < stay; j0 += gridDim.z * kBlock) {
-            const int j = j0 + threadIdx.x;
+    } else {
+        for (int j0 = blockIdx.z * kBlock; j0 < a.keep; j0 += gridDim.z * kBlock) {
+            const int j = j0 + threadIdx.x, s = from(j);
             int64_t w = 0;
-            if (j < stay) w = weight_at(c, b, h, min(max(kept[j], 0), n - 1));
+            if (s >= 0) w = *weight_slot(c, b, h, s);
             __syncthreads();
-            const int to = j < stay ? target(j) : -1;
+            const int to = s >= 0 ? target(j) : -1;
             if (to >= 0) c.weight[(((int64_t)to * c.Hkv + h) << c.log2_page) + (j & (page - 1))] = w;
         }
     }
-}
-
-// After the moves: they read the lengths.
-__global__ __launch_bounds__(kBlock) void evict_length_kernel(EvictArgs a) {
-    const int b = blockIdx.x * kBlock + threadIdx.x;
-    if (b < a.c.B) a.length_out[b] = min(keys_of(a.c, b), a.keep);
 }
 
 }  // namespace
@@ -345,14 +400,16 @@ hipError_t launch_kv_evict(const EvictArgs& a, hipStream_t stream) {
     const CacheView& c = a.c;
     const LaunchEvents ev = launch_events();
     set_launch_events(ev.start, nullptr);
-    launch_kernel(evict_select_kernel, dim3(c.Hkv, c.B), dim3(kSelect), 0, stream, a);
-    set_launch_events(nullptr, nullptr);
+    const int64_t most = (int64_t)c.max_pages << c.log2_page;
+    const dim3 units(c.Hkv, c.B);
+    if (most <= 8 * kSelect) launch_kernel(evict_select_kernel<8>, units, dim3(kSelect), 0, stream, a);
+    else if (most <= 32 * kSelect) launch_kernel(evict_select_kernel<32>, units, dim3(kSelect), 0, stream, a);
+    else launch_kernel(evict_select_kernel<0>, units, dim3(kSelect), 0, stream, a);
+    set_launch_events(nullptr, ev.stop);
     // in place the tiles of a workgroup follow one another
     const int tiles = a.table_out == c.table ? 1 : (a.keep + kBlock - 1) / kBlock;
     launch_kernel(evict_move_kernel, dim3((2 + (c.d >> 4)) * c.Hkv, c.B, tiles < 16 ? tiles : 16),
                   dim3(kBlock), 0, stream, a);
-    set_launch_events(nullptr, ev.stop);
-    launch_kernel(evict_length_kernel, dim3((c.B + kBlock - 1) / kBlock), dim3(kBlock), 0, stream, a);
     return hipGetLastError();
 }
 

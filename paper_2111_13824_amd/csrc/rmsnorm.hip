@@ -59,6 +59,30 @@ typedef int8_t i8x8 __attribute__((ext_vector_type(8)));
 typedef uint8_t u8x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// The factors of a group's channels (0 beyond C).
+template <int LANES, bool VEC>
+__device__ __forceinline__ void load_gamma(const float* p, int lane, int j, int C, float (&out)[8]) {
+    if (VEC) {
+        const int c = place<LANES, true>(lane, j, 0);
+        f32x4 g0 = {0.0f, 0.0f, 0.0f, 0.0f}, g1 = g0;
+        if (c < C) {
+            g0 = *reinterpret_cast<const f32x4*>(p + c);
+            g1 = *reinterpret_cast<const f32x4*>(p + c + 4);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            out[e] = g0[e];
+            out[4 + e] = g1[e];
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = place<LANES, false>(lane, j, e);
+            out[e] = c < C ? p[c] : 0.0f;
+        }
+    }
+}
+
 // Values at and beyond C are skipped.
 template <int LANES, bool VEC, typename T, typename V8>
 __device__ __forceinline__ void load8(const T* p, int lane, int j, int C, T (&out)[8]) {
@@ -110,7 +134,10 @@ __global__ __launch_bounds__(kBlock) void rmsnorm_kernel(RmsArgs a) {
     const int C = a.C;
 
     int h[NV][8];
+    float gamma[NV][8];
     uint64_t m2 = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) load_gamma<LANES, VEC>(a.gamma, lane, j, C, gamma[j]);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         int16_t r[8] = {};
@@ -148,16 +175,15 @@ __global__ __launch_bounds__(kBlock) void rmsnorm_kernel(RmsArgs a) {
 
     const int half = 1 << (a.bits - 1);
     const float lo = (float)-half, hi = (float)(half - 1);
-    float f[NV][8], add = kMagic, factor = 0.0f;
+    float add = kMagic, factor = 0.0f;
     if (ROWS) {
         float top = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int c = place<LANES, VEC>(lane, j, e);
-                f[j][e] = c < C ? a.gamma[c] * (float)h[j][e] : 0.0f;
-                top = fmaxf(top, fabsf(f[j][e]));
+                gamma[j][e] *= (float)h[j][e];          // a
+                top = fmaxf(top, fabsf(gamma[j][e]));
             }
         top = row_max<LANES>(top, tops);
         factor = top > 0.0f ? (float)((double)hi / (double)top) : 0.0f;
@@ -173,13 +199,8 @@ __global__ __launch_bounds__(kBlock) void rmsnorm_kernel(RmsArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             float t;
-            if (ROWS) {
-                t = __builtin_fmaf(f[j][e], factor, add);
-            } else {
-                const int c = place<LANES, VEC>(lane, j, e);
-                const float g = c < C ? a.gamma[c] * factor : 0.0f;
-                t = __builtin_fmaf((float)h[j][e], g, add);
-            }
+            if (ROWS) t = __builtin_fmaf(gamma[j][e], factor, add);
+            else t = __builtin_fmaf((float)h[j][e], gamma[j][e] * factor, add);
             o[e] = (int8_t)(int)fminf(fmaxf(t - kMagic, lo), hi);
         }
         store8<LANES, VEC, int8_t, i8x8>(a.y + base, lane, j, C, o);
@@ -203,7 +224,7 @@ void launch(const RmsArgs& a, bool vec, hipStream_t stream) {
 hipError_t launch_rmsnorm(const RmsArgs& a, hipStream_t stream) {
     const auto aligned = [](const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; };
     const bool vec = a.C % 8 == 0 && aligned(a.r, 16) && aligned(a.h, 16) && aligned(a.x, 8) &&
-                     aligned(a.alpha, 8) && aligned(a.y, 8);
+                     aligned(a.alpha, 8) && aligned(a.y, 8) && aligned(a.gamma, 16);
     if (a.C <= 32) launch<4, 1>(a, vec, stream);
     else if (a.C <= 128) launch<16, 1>(a, vec, stream);
     else if (a.C <= 512) launch<64, 1>(a, vec, stream);
