@@ -1028,7 +1028,7 @@ void launch(const PagedArgs& a, const Shape& sh, const Plan& p, hipStream_t stre
 }  // namespace
 
 #if defined(FQ_PAGED_32)
-void launch_lis_paged_32(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<1, 4, 1, 1, 2>, Config<1, 1, 8, 1, 2>>(a, sh, p, s); }
+void launch_lis_paged_32(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<2, 2, 2, 1, 2>, Config<1, 1, 8, 1, 2>>(a, sh, p, s); }
 #elif defined(FQ_PAGED_64)
 void launch_lis_paged_64(const PagedArgs& a, const paged::Shape& sh, const paged::Plan& p, hipStream_t s) { launch<Config<1, 4, 1, 1, 4>, Config<1, 1, 8, 1, 4>>(a, sh, p, s); }
 #elif defined(FQ_PAGED_128)

@@ -172,6 +172,14 @@ ATTEND = [
     (1, 2, 2, 2, 64, 64, [3000], [2], dict(flat=True)),
     (1, 2, 2, 2, 64, 64, [900], [2], dict(spread=127.0, s=2e-4, n=14)),
     (33, 2, 1, 1, 64, 16, list(range(33)), [1] * 33, {}),
+    # keys in parts: many rows and few, wide heads, parts that hold nothing, general scales
+    (1, 4, 2, 20, 64, 64, [5000], [20], {}),
+    (2, 2, 1, 40, 128, 32, [4100, 70], [40, 33], dict(zp_q=-2, zp_v=1)),
+    (1, 2, 1, 9, 32, 16, [3001], [9], dict(s=2e-4, n=14)),
+    (2, 16, 2, 2, 96, 16, [2100, 1], [2, 1], dict(bits=3)),
+    (1, 16, 1, 1, 64, 128, [3000], [1], dict(s=2e-4, n=14, zp_q=-128, zp_v=5)),
+    (3, 8, 1, 2, 128, 64, [2049, 0, 1500], [2, 2, 0], dict(causal=False)),
+    (65, 2, 1, 2, 16, 16, [3 * i % 50 for i in range(65)], [2] * 65, {}),
 ]
 
 
@@ -200,6 +208,11 @@ EVICT = [
     (2, 2, 112, 1024, [2048, 7], 2048, 5, "any"),
     (1, 2, 64, 32, [2049], 2048, 2047, "few"),
     (2, 2, 96, 16, [700, 650], 350, 10, "signs"),
+    # more keys than a workgroup holds at once in eight and in 32 registers a thread
+    (1, 2, 16, 16, [9000], 5000, 700, "any"),
+    (1, 1, 16, 64, [20000], 300, 0, "few"),
+    (1, 1, 16, 1024, [40000], 33000, 2, "signs"),
+    (1, 1, 16, 64, [35001], 100, 99, "equal"),
 ]
 
 
