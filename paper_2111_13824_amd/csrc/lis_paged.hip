@@ -86,12 +86,12 @@ struct Place {
     int64_t unit;
 };
 
-// PARTS: a call whose rows are few and whose keys are divided: a unit's parts, which add to
-// the same few results, stay on one or two XCDs.
-template <bool PARTS>
+// FEW: at most 16 rows, whose workgroups start together or nearly; of divided keys a unit's
+// parts, which add to the same few results, stay on one or two XCDs.
+template <bool FEW>
 __device__ __forceinline__ Place place_of(const PagedArgs& a, const Shape& sh, int lane) {
     // fewer than 2^24 workgroups: 32-bit divisions
-    if (PARTS) {
+    if (FEW) {
         const uint32_t block = (uint32_t)lis::xcd_remap(blockIdx.x, gridDim.x);
         const uint32_t u = block / (uint32_t)sh.splits;
         Place p;
@@ -491,11 +491,19 @@ struct Config {
     static constexpr int threads = 64 * RG * KG, rows = 16 * RS * RG;
 };
 
-// A sum over the lanes of a wavefront.
+// A sum over the lanes of a wavefront: rotations within 16 lanes, then lane swaps.
+template <int CTRL>
+__device__ __forceinline__ uint64_t rotated(uint64_t v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, 0xF, 0xF, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, 0xF, 0xF, true);
+    return ((uint64_t)hi << 32) | lo;
+}
 __device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-    return v;
+    v += rotated<0x128>(v);
+    v += rotated<0x124>(v);
+    v += rotated<0x122>(v);
+    v += rotated<0x121>(v);
+    return lis::row4_sum(v);
 }
 
 // The I-Exp values of four stored logits of a row of maximum mx, those at `end` and behind left out.
@@ -522,15 +530,23 @@ __device__ __forceinline__ uint64_t sum4(i32x4 v, int key0, int end, int mx, con
     return sum;
 }
 
-// f(row, key, end) for the rows and runs of 256 keys of [from, to), a wavefront a run, every lane
-// its four keys from `key` on; the row sees the keys before `end`.
-template <typename F>
-__device__ __forceinline__ void for_row_runs(const PagedArgs& a, int len, int fresh, int rows, int from, int to,
-                                             int lane, int wave, int waves, F&& f) {
-    const int runs = (to - from + 255) / 256;
-    for (int at = wave; at < rows * runs; at += waves) {
-        const int row = at / runs;
-        f(row, from + 256 * (at - row * runs) + 4 * lane, min(to, limit_of(a, len, fresh, row)));
+// Sums of stored logits: a wavefront takes runs of 256 keys of [from, to) of one row after
+// another, every lane four keys of each; rows fewer than the wavefronts are shared by
+// them.  done(row, sum): of what the wavefront took.  logits(row): the row's.
+template <bool FAST, typename L, typename F>
+__device__ __forceinline__ void sum_rows(const PagedArgs& a, int len, int fresh, int rows, int from, int to,
+                                         int lane, int wave, int waves, const int* row_max, L&& logits, F&& done) {
+    const int share = rows < waves ? waves / rows : 1;          // wavefronts a row
+    const int first = share > 1 ? wave % rows : wave, part = share > 1 ? wave / rows : 0;
+    if (part >= share) return;
+    for (int row = first; row < rows; row += waves) {
+        const int end = min(to, limit_of(a, len, fresh, row)), mx = row_max[row];
+        const auto* p = logits(row);
+        uint64_t sum = 0;
+        for (int key = from + 256 * part + 4 * lane; key < end; key += 256 * share)
+            sum += sum4<FAST>(*reinterpret_cast<const i32x4*>(p + key), key, end, mx, a);
+        sum = wave_sum(sum);
+        if (lane == 0) done(row, sum);
     }
 }
 
@@ -561,7 +577,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rg = wave % RG, kg = wave / RG;
-    const Place at = place_of<KEEP == kWorkspace>(a, sh, lane);
+    const Place at = place_of<KEEP != kNot>(a, sh, lane);
     const int split = at.split, tile = at.tile, b = at.b, h = at.h;
     const int64_t unit = at.unit;
     const int len = keys_of(a.c, b);
@@ -608,13 +624,11 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     const auto prime = [&](auto with_keys, auto with_values) {
         constexpr bool K = decltype(with_keys)::value, V = decltype(with_values)::value;
         if (stages == 0) return;
-        next = st.blocks(from);
-        st.template load<K, V>(next, r[0]);
-        next = st.blocks(from + step);
-        if (sets(with_values) == 2) {
-            st.template load<K, V>(next, r[1]);
-            next = st.blocks(from + 2 * step);
-        }
+        const auto b0 = st.blocks(from), b1 = st.blocks(from + step);
+        next = st.blocks(from + 2 * step);
+        st.template load<K, V>(b0, r[0]);
+        if (sets(with_values) == 2) st.template load<K, V>(b1, r[1]);
+        else next = b1;
     };
     const auto walk = [&](const i32x4 (&add)[RS], auto with_keys, auto with_values, auto&& body) {
         constexpr bool K = decltype(with_keys)::value, V = decltype(with_values)::value;
@@ -758,14 +772,9 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     if (PASS == kAll || PASS == kSum) {
         if (KEEP == kLds) {
             prime(No{}, Yes{});
-            for_row_runs(a, len, fresh, rows, from, until, lane, wave, KG * RG, [&](int row, int key0, int end) {
-                uint64_t v = 0;
-                if (key0 < end)
-                    v = sum4<FAST>(*reinterpret_cast<const i32x4*>(lds_logits + row * (int)sh.keys + key0), key0, end,
-                                   row_max[row], a);
-                v = wave_sum(v);
-                if (lane == 0) atomicAdd(&row_sum[row], (unsigned long long)v);
-            });
+            sum_rows<FAST>(a, len, fresh, rows, from, until, lane, wave, KG * RG, row_max,
+                           [&](int row) { return lds_logits + row * (int)sh.keys; },
+                           [&](int row, uint64_t v) { atomicAdd(&row_sum[row], (unsigned long long)v); });
         } else {
         if (PASS == kAll) prime(Yes{}, No{});
         RowAdder<MODE> sum[RS];
@@ -958,13 +967,9 @@ __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shap
     __syncthreads();
     if (split == 0 && threadIdx.x < rows) sh.row_max[row_at + threadIdx.x] = row_max[threadIdx.x];
     const int32_t* lg = sh.logits + unit * sh.rows * sh.keys;
-    for_row_runs(a, len, fresh, rows, from, to, lane, wave, kBlock / 64, [&](int row, int key0, int end) {
-        uint64_t v = 0;
-        if (key0 < end)
-            v = sum4<FAST>(*reinterpret_cast<const i32x4*>(lg + row * sh.keys + key0), key0, end, row_max[row], a);
-        v = wave_sum(v);
-        if (lane == 0) atomicAdd(&row_sum[row], (unsigned long long)v);
-    });
+    sum_rows<FAST>(a, len, fresh, rows, from, to, lane, wave, kBlock / 64, row_max,
+                   [&](int row) { return lg + row * sh.keys; },
+                   [&](int row, uint64_t v) { atomicAdd(&row_sum[row], (unsigned long long)v); });
     __syncthreads();
     if (threadIdx.x < rows)
         atomicAdd(reinterpret_cast<unsigned long long*>(sh.row_sum) + row_at + threadIdx.x, row_sum[threadIdx.x]);

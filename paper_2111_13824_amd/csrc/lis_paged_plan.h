@@ -59,11 +59,15 @@ inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int64_t max_keys
         p.way = kOneFew;
         return p;
     }
-    // parts of at least 1024 keys until there are two workgroups a compute unit
+    // Parts until there are two workgroups a compute unit: of at least two stages of few
+    // rows (1024 keys), and where the tiles come one by one of four (256 keys).
     int64_t want = 512 / (groups > 0 ? groups : 1);
-    if (want > p.keys / 1024) want = p.keys / 1024;
+    const int64_t most = p.keys / (p.rows <= 16 ? 1024 : 256);
+    if (want > most) want = most;
     if (want > 256) want = 256;
     if (want > 1) p.splits = (int32_t)want;
+    // three launches cost what four tiles in a row do: chunks of few keys stay in one
+    if (p.rows > 16 && p.keys < 1024) p.splits = 1;
     p.way = p.rows <= 16 ? kPartsFew : (p.splits > 1 ? kParts : kOne);
     return p;
 }
