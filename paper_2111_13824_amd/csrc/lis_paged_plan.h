@@ -55,14 +55,18 @@ inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int64_t max_keys
     p.tile_rows = p.rows <= 16 ? 16 : 64;
     p.tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
     const int64_t groups = p.units * p.tiles;
-    if (p.rows <= 16 && p.rows * p.keys <= kLdsLogits) {
+    // One launch of a workgroup a unit takes 4 us and 2 more for every 512 keys, three launches
+    // 18 to some thousands of keys; with workgroups for half the compute units they are even
+    // (4 units of 1024, 2048 and 4096 keys: 12, 16 and 24 us to 18).
+    if (p.rows <= 16 && p.rows * p.keys <= kLdsLogits && (p.keys <= 2048 || p.units >= 128)) {
         p.way = kOneFew;
         return p;
     }
-    // Parts until there are two workgroups a compute unit: of at least two stages of few
-    // rows (1024 keys), and where the tiles come one by one of four (256 keys).
-    int64_t want = 512 / (groups > 0 ? groups : 1);
-    const int64_t most = p.keys / (p.rows <= 16 ? 1024 : 256);
+    // Parts until every compute unit has a workgroup (two, of chunks): of a stage of few rows
+    // (512 keys), of four tiles where they come one by one (256).  Twice the parts of few
+    // rows cost more than they hide (each adds to the results: 131072 keys, 58 us for 49).
+    int64_t want = (p.rows <= 16 ? 256 : 512) / (groups > 0 ? groups : 1);
+    const int64_t most = p.keys / (p.rows <= 16 ? 512 : 256);
     if (want > most) want = most;
     if (want > 256) want = 256;
     if (want > 1) p.splits = (int32_t)want;
