@@ -12,9 +12,10 @@
 // the cache holds values with their channels in rows.
 //
 // Tiles of keys and values come into LDS in the order of memory, a stage of a few tiles at
-// a time, loaded three stages ahead; a workgroup's wavefronts share them.  (Loaded straight into the operands' registers,
-// 16 neighbouring lanes read 16 rows: the chunks of 8 x 16 heads x 512 tokens over 4096
-// keys took 214 us, of which the vector instructions were a third.)
+// a time: two stages there, two more on their way in registers.  A workgroup's wavefronts
+// share them.  (Loaded straight into the operands' registers, 16 neighbouring lanes read 16
+// rows: 8 chunks of 16 heads over up to 4096 keys took 214 us, 167 so; vector
+// instructions were a third of the former.)
 //
 // A weight P = 2^m, m = (2^b - 1) - code in [0, 15], is not an int8: it is taken as
 // -256 hi - lo with hi, lo in {0, -1, -2, .. -128}, two products with the same V
@@ -161,41 +162,55 @@ struct Stage {
     static_assert(kKeyLoads * RG == 4 * KS && kValueLoads * RG == NV, "parts are whole loads");
 
     // Pages of the tile's blocks of 16 keys and the blocks' first slots in them (pages of 64
-    // keys and more: the first block's, which hold for all): uniform values, read
-    // through the scalar cache a stage ahead.
+    // keys and more: the first block's, which hold for all): uniform values.
     struct Blocks {
         int id[4], off[4];
     };
 
     const PagedArgs& a;
-    int b, h, len, lane, wave;
+    int b, h, len, from, lane, wave;
     bool whole;                 // a page holds whole tiles
     int64_t head;               // bytes before the head in a page
     uint32_t stride;            // bytes of a page (at most 2^27)
+    // Pages of 16 stages, block lane % 4 of stage lane / 4: the first ones, those that loads
+    // are sent for, and the next.  (Scalar loads of a stage's, which the compiler moved to
+    // right before their use: one token of 64 streams of 4096 keys 32.3 us, 30.3 so.)
+    int first, now, then;
 
-    __device__ __forceinline__ Blocks blocks(int key0) const {
-        typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
-        const scalar_ptr table = (scalar_ptr)(a.c.table + (int64_t)b * a.c.max_pages);
-        const int tile0 = key0 + 64 * (wave / RG);
+    __device__ __forceinline__ int key_of(int n) const { return from + 64 * (KG * n + wave / RG); }
+
+    // an id that is no page of the cache reads as page 0
+    __device__ __forceinline__ int ids(int n) const {
+        const int at = min(key_of(n + (lane >> 2)) + 16 * (lane & 3), (len - 1) & ~15);     // behind the last: it again
+        const int id = a.c.table[(int64_t)b * a.c.max_pages + (at >> a.c.log2_page)];
+        return (uint32_t)id < (uint32_t)a.c.pages ? id : 0;
+    }
+    __device__ __forceinline__ void begin() {
+        now = first;
+        then = ids(16);
+    }
+    // n from 0 on, one after another
+    __device__ __forceinline__ Blocks blocks(int n) {
+        if (n > 0 && (n & 15) == 0) {
+            now = then;
+            then = ids(n + 16);
+        }
+        const int mask = (1 << a.c.log2_page) - 1, key0 = key_of(n), i = 4 * (n & 15);
         Blocks t;
         if (whole) {
-            const int at = min(tile0, (len - 1) & ~63);         // behind the last tile: it again
-            t.id[0] = table[at >> a.c.log2_page];
-            t.off[0] = at & ((1 << a.c.log2_page) - 1);
+            t.id[0] = __builtin_amdgcn_readlane(now, i);
+            t.off[0] = min(key0, (len - 1) & ~63) & mask;
         } else {
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                const int at = min(tile0 + 16 * p, (len - 1) & ~15);
-                t.id[p] = table[at >> a.c.log2_page];
-                t.off[p] = at & ((1 << a.c.log2_page) - 1);
+                t.id[p] = __builtin_amdgcn_readlane(now, i + p);
+                t.off[p] = min(key0 + 16 * p, (len - 1) & ~15) & mask;
             }
         }
         return t;
     }
-    // the head's first byte in a page; an id that is no page of the cache reads as page 0
-    __device__ __forceinline__ int64_t base(int id) const {
-        return head + (int64_t)((uint64_t)((uint32_t)id < (uint32_t)a.c.pages ? (uint32_t)id : 0u) * stride);
-    }
+    // the head's first byte in a page
+    __device__ __forceinline__ int64_t base(int id) const { return head + (int64_t)((uint64_t)(uint32_t)id * stride); }
 
     // A stage on its way.
     struct Loads {
@@ -602,7 +617,8 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
 
     Queries<RS, KS> q;
     const int64_t head_bytes = (int64_t)a.c.d << a.c.log2_page;
-    const St st{a, b, h, len, lane, wave, a.c.log2_page >= 6, h * head_bytes, (uint32_t)(a.c.Hkv * head_bytes)};
+    St st{a, b, h, len, from, lane, wave, a.c.log2_page >= 6, h * head_bytes, (uint32_t)(a.c.Hkv * head_bytes)};
+    if (stages > 0) st.first = st.ids(0);
     if (KEYS) q.load(a, b, h, min(row0, rows - 1), rows, lane);
     // the lane's row of the logits that are kept
     int32_t* const lds_logits = reinterpret_cast<int32_t*>(dyn + (FAST ? tile_rows * 4 * sh.buckets : 0));
@@ -616,7 +632,6 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     // where they are.
     constexpr int step = KG * kTile;
     typename St::Loads r[2];
-    typename St::Blocks next;
     // How many stages are on their way beside the two in LDS: values of wide heads, which a
     // wavefront of few rows loads alone, leave registers for one.
     const auto sets = [](auto values) { return decltype(values)::value && NV == 8 && RG == 1 ? 1 : 2; };
@@ -624,11 +639,9 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     const auto prime = [&](auto with_keys, auto with_values) {
         constexpr bool K = decltype(with_keys)::value, V = decltype(with_values)::value;
         if (stages == 0) return;
-        const auto b0 = st.blocks(from), b1 = st.blocks(from + step);
-        next = st.blocks(from + 2 * step);
-        st.template load<K, V>(b0, r[0]);
-        if (sets(with_values) == 2) st.template load<K, V>(b1, r[1]);
-        else next = b1;
+        st.begin();
+        st.template load<K, V>(st.blocks(0), r[0]);
+        if (sets(with_values) == 2) st.template load<K, V>(st.blocks(1), r[1]);
     };
     const auto walk = [&](const i32x4 (&add)[RS], auto with_keys, auto with_values, auto&& body) {
         constexpr bool K = decltype(with_keys)::value, V = decltype(with_values)::value;
@@ -636,8 +649,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
         if (stages == 0) return;
         const int own = from + kg * kTile;
         st.template store<K, V>(r[0], stage_k[0], stage_v(0));
-        st.template load<K, V>(next, r[0]);
-        next = st.blocks(from + (kSets + 1) * step);
+        st.template load<K, V>(st.blocks(kSets), r[0]);
         meet();
         const auto stored = [&](int key0, i32x4 (&acc)[RS][4]) {
             const int k = min(key0, (int)sh.keys - kTile);
@@ -648,13 +660,41 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
         };
         i32x4 ahead[RS][4];
         if (!K && KEEP == kWorkspace) stored(own, ahead);
-        // stage n, of parity i: stage n + 1 goes into LDS, the next that is not on its way is
+        const auto visit = [&](int key0, i32x4 (&acc)[RS][4], const int8_t* values) {
+            const bool edge = key0 + kTile > whole;
+            if (edge) {
+#pragma unroll
+                for (int s = 0; s < RS; ++s) {
+                    const int n_seen = seen(key0, min(limit[s], to), lane);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) acc[s][t][x] = 4 * t + x < n_seen ? acc[s][t][x] : INT_MIN;
+                }
+            }
+            body(key0, acc, values, edge);
+        };
+        // Passes over keys alone that keep nothing take the logits a stage ahead of their use,
+        // and the keys come into LDS two stages ahead: reads and products hide behind
+        // the vector instructions (8 chunks of 16 heads over up to 4096 keys 145 us, 143 so;
+        // 154 and 149 from memory).  The last pass has no registers for it.
+        constexpr bool AHEAD = K && !V && KEEP == kNot;
+        i32x4 two[2][RS][4];
+        Operand<KS> k[4];
+        if (AHEAD) {
+            st.template store<K, V>(r[1], stage_k[1], stage_v(1));
+            st.template load<K, V>(st.blocks(3), r[1]);
+            st.read_k(stage_k[0], k);
+            q.template logits<FAST>(k, add, two[0]);
+            meet();
+        }
+        // stage n, of parity i: the next one goes into LDS, the next that is not on its way is
         // sent for
         const auto stage = [&](int n, auto i_, auto works) {
-            constexpr int i = decltype(i_)::value, o = kSets == 2 ? i ^ 1 : 0;
+            constexpr int i = decltype(i_)::value, into = AHEAD ? i : i ^ 1, o = kSets == 2 ? into : 0;
             const int key0 = own + n * step;
+            st.template store<K, V>(r[o], stage_k[into], stage_v(into));
             i32x4 acc[RS][4];
-            st.template store<K, V>(r[o], stage_k[i ^ 1], stage_v(i ^ 1));
             if (!K) {
                 if (KEEP == kLds) {
                     stored(key0, acc);
@@ -664,29 +704,22 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
                     stored(key0 + step, ahead);
                 }
             }
-            st.template load<K, V>(next, r[o]);
-            next = st.blocks(from + (n + kSets + 2) * step);
+            st.template load<K, V>(st.blocks(n + kSets + (AHEAD ? 2 : 1)), r[o]);
             if (decltype(works)::value) {
-                if (K) {
-                    Operand<KS> k[4];
-                    st.read_k(stage_k[i], k);
-                    q.template logits<FAST>(k, add, acc);
+                if constexpr (AHEAD) {
+                    st.read_k(stage_k[i ^ 1], k);
+                    visit(key0, two[i], stage_v(i));
+                    q.template logits<FAST>(k, add, two[i ^ 1]);
                 } else {
+                    if (K) {
+                        st.read_k(stage_k[i], k);
+                        q.template logits<FAST>(k, add, acc);
+                    } else {
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) acc[0][t] += add[0];
-                }
-                const bool edge = key0 + kTile > whole;
-                if (edge) {
-#pragma unroll
-                    for (int s = 0; s < RS; ++s) {
-                        const int n_seen = seen(key0, min(limit[s], to), lane);
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) acc[s][t][x] = 4 * t + x < n_seen ? acc[s][t][x] : INT_MIN;
+                        for (int t = 0; t < 4; ++t) acc[0][t] += add[0];
                     }
+                    visit(key0, acc, stage_v(i));
                 }
-                body(key0, acc, stage_v(i), edge);
             }
             meet();
         };
@@ -776,22 +809,22 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
                            [&](int row) { return lds_logits + row * (int)sh.keys; },
                            [&](int row, uint64_t v) { atomicAdd(&row_sum[row], (unsigned long long)v); });
         } else {
-        if (PASS == kAll) prime(Yes{}, No{});
-        RowAdder<MODE> sum[RS];
+            if (PASS == kAll) prime(Yes{}, No{});
+            RowAdder<MODE> sum[RS];
 #pragma unroll
-        for (int s = 0; s < RS; ++s) add[s] = splat(FAST ? -lis::screen_c(mx[s], a.k) : 0);
-        walk(add, Yes{}, No{}, [&](int key0, const i32x4 (&acc)[RS][4], const int8_t*, bool edge) {
+            for (int s = 0; s < RS; ++s) add[s] = splat(FAST ? -lis::screen_c(mx[s], a.k) : 0);
+            walk(add, Yes{}, No{}, [&](int key0, const i32x4 (&acc)[RS][4], const int8_t*, bool edge) {
 #pragma unroll
-            for (int s = 0; s < RS; ++s) sum[s].add(acc[s], mx[s], a);
-            if (edge)
+                for (int s = 0; s < RS; ++s) sum[s].add(acc[s], mx[s], a);
+                if (edge)
 #pragma unroll
-                for (int s = 0; s < RS; ++s) sum[s].take_off(16 - seen(key0, min(limit[s], to), lane), a);
-        });
+                    for (int s = 0; s < RS; ++s) sum[s].take_off(16 - seen(key0, min(limit[s], to), lane), a);
+            });
 #pragma unroll
-        for (int s = 0; s < RS; ++s) {
-            const uint64_t v = lis::row4_sum(sum[s].sum);
-            if (lane < 16) atomicAdd(&row_sum[rg * kRows + 16 * s + lane], (unsigned long long)v);
-        }
+            for (int s = 0; s < RS; ++s) {
+                const uint64_t v = lis::row4_sum(sum[s].sum);
+                if (lane < 16) atomicAdd(&row_sum[rg * kRows + 16 * s + lane], (unsigned long long)v);
+            }
         }
         __syncthreads();
         if (PASS == kSum) {
@@ -884,18 +917,10 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
         }
         if (WEIGHT) {
             const uint32_t sum = sum16(got, lane);          // of key lane % 16 of the lane's block
-            const auto t = st.blocks(key0 - kg * kTile);
-            const int g = lane >> 4;
-            int64_t slot;
-            if (st.whole) {
-                slot = ((int64_t)((uint32_t)t.id[0] < (uint32_t)a.c.pages ? t.id[0] : 0) * a.c.Hkv + h) << a.c.log2_page;
-                slot += t.off[0] + 16 * g;
-            } else {
-                const int id = g & 2 ? (g & 1 ? t.id[3] : t.id[2]) : (g & 1 ? t.id[1] : t.id[0]);
-                const int off = g & 2 ? (g & 1 ? t.off[3] : t.off[2]) : (g & 1 ? t.off[1] : t.off[0]);
-                slot = ((int64_t)((uint32_t)id < (uint32_t)a.c.pages ? id : 0) * a.c.Hkv + h) << a.c.log2_page;
-                slot += off;
-            }
+            const int at = min(key0 + 16 * (lane >> 4), (len - 1) & ~15);
+            const int id = a.c.table[(int64_t)b * a.c.max_pages + (at >> a.c.log2_page)];
+            const int64_t slot = (((int64_t)((uint32_t)id < (uint32_t)a.c.pages ? id : 0) * a.c.Hkv + h) << a.c.log2_page) +
+                                 (at & ((1 << a.c.log2_page) - 1));
             if (sum) atomicAdd(reinterpret_cast<unsigned long long*>(a.c.weight) + slot + (lane & 15), (unsigned long long)sum);
         }
     };
