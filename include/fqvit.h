@@ -591,9 +591,10 @@ fq_status lis_attention_paged(const int8_t* q, int32_t B, int32_t Hq, int32_t Hk
  * places [0, keep) of the pages that table_out names.
  *
  *   keep    in [1, 2^20]; recent in [0, keep].
- *   table_out  [B, max_out] int32, max_out page >= keep: table itself (in place, with
- *           max_out = max_pages) or pages that no other sequence's entries of
- *           either table name.  In place, a sequence's pages are its own.
+ *   table_out  [B, max_out] int32, max_out page >= keep: table itself (then max_out =
+ *           max_pages), or for each sequence the first entries of its row of table
+ *           (in place: the sequence's pages are its own) or pages that nothing else in
+ *           either table names.
  *   length_out [B] int32 (out): min(length, keep); it may be length itself.
  *   kept    [B, Hkv, keep] int32 (out): the places that stayed, ascending; -1 behind the last.
  *           A sequence of at most `keep` keys keeps them all (in other pages: is copied).

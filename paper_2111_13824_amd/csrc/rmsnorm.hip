@@ -1,6 +1,9 @@
 // Root-mean-square norm of an int16 stream with an int8 branch added to it, for
 // gfx950.  Memory-bound: 6 bytes a value (branch 1, stream 2 read and 2 written,
-// output 1).
+// output 1), all of them once: a row's values stay in the registers of a group of lanes, a
+// wavefront up to 1024 channels and a workgroup above.  9232 x 1024: 12.1 us, 4.7 TB/s (a
+// copy reaches 5.2); with the factors loaded one by one 25.5.  One row: 2.8 us of a call
+// of 9.5.
 //
 //   h = clip16(r + rint((x - zp_x) 2^min(alpha, K) m_x)),  M2 = sum h^2
 //   rho = 1 / sqrt(M2 / C + eps)  (binary64, each operation rounded once)

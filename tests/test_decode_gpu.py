@@ -200,3 +200,18 @@ def test_evict(fq, case):  # noqa: F811
         for got, want in zip((*on, n_out, kept), ref):
             assert np.array_equal(host(got), want)
         assert np.array_equal(host(n), length if elsewhere else ref[3])
+
+
+def test_evict_in_place_through_another_table(fq):  # noqa: F811
+    """table_out with the first entries of table, in memory of its own, for one sequence,
+    and other pages for the other: many tiles of places, of which those in place have
+    to follow one another."""
+    c, length, keep, recent, to = R.evict_case((2, 2, 64, 32, [2800, 2500], 1900, 60, "any"))
+    to[0] = c["table"][0]
+    pages = -(-keep // 32)
+    to = np.ascontiguousarray(to[:, :pages])
+    on = [dev(c[n]) for n in ("k", "v", "weight")]
+    n_out, kept = fq.kv_cache_evict(*on, dev(c["table"]), dev(length), keep, recent, table_out=dev(to))
+    ref = R.evict(c, length, keep, recent, to)
+    for got, want in zip((*on, n_out, kept), ref):
+        assert np.array_equal(host(got), want)
