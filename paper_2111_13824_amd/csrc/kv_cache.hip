@@ -159,6 +159,7 @@ namespace {
 
 constexpr int kSelect = 1024;
 constexpr int kSelectWaves = kSelect / 64;
+constexpr int kCopies = 8;
 
 // Order of signed weights as unsigned numbers.
 __device__ __forceinline__ uint64_t rank_of(int64_t w) { return (uint64_t)w ^ (1ull << 63); }
@@ -174,10 +175,12 @@ __device__ __forceinline__ const int64_t* weight_slot(const CacheView& c, int b,
 // one wavefront takes) from the first bit in which the weights differ; then one scan
 // over the threads places what is heavier and as many of its equals, from the lowest
 // place on, as are missing.  (A histogram that one thread walks takes 10 us a digit.)
-// Bound by the digits' barriers, some 2 us each: 128 units of up to 8192 weights, 5 MB, 14.5 us.
+// Bound by the digits' passes, some 2 us each: 128 units of up to 8192 weights, 5 MB, 12.8 us;
+// 14.5 with one histogram, whose first bins' additions, weights of all sizes in them,
+// wait for each other.
 template <int ITEMS>
 __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
-    __shared__ uint32_t hist[256];
+    __shared__ uint32_t hist[kCopies][257];     // copies begin in different banks
     __shared__ uint64_t wide[kSelectWaves];
     __shared__ uint32_t part[2][kSelectWaves];
     __shared__ uint64_t bound;
@@ -239,16 +242,21 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
     for (int hi = top; hi > 0;) {
         const int lo = max(hi - 8, 0);
         const uint32_t mask = (1u << (hi - lo)) - 1;
-        if (tid < 256) hist[tid] = 0;
+        for (int i = tid; i < kCopies * 257; i += kSelect) (&hist[0][0])[i] = 0;
         __syncthreads();
         each([&](uint64_t w) {
-            if (hi == 64 || (w >> hi) == (prefix >> hi)) atomicAdd(&hist[(uint32_t)(w >> lo) & mask], 1u);
+            if (hi == 64 || (w >> hi) == (prefix >> hi)) atomicAdd(&hist[lane % kCopies][(uint32_t)(w >> lo) & mask], 1u);
         });
         __syncthreads();
         if (wave == 0) {        // the digit of the need-th heaviest: lane l holds the bins 255 - 4 l and below
             uint32_t v[4], sum = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += v[e] = hist[255 - 4 * lane - e];
+            for (int e = 0; e < 4; ++e) {
+                v[e] = 0;
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i) v[e] += hist[i][255 - 4 * lane - e];
+                sum += v[e];
+            }
             uint32_t before = sum;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {

@@ -26,7 +26,7 @@
 // them less than one vector instruction), so each pass takes the logits again; a call
 // of at most 16 rows a key head, which the keys' bytes bound, stores them instead.
 //
-// Measured.  Chunks (8 of up to 512 tokens and 16 heads of 64, 4096 keys): 143 us, 36 GOP;
+// Measured.  Chunks (8 of up to 512 tokens and 16 heads of 64, 4096 keys): 140 us, 36 GOP;
 // bound by vector instructions, 41 million for the codes and sums, a compute unit busy 70 % of
 // the time (maximum 18 us, sum 44, codes and product 38, and the shorter sequences'
 // workgroups end before the longest).  One token of 64 streams (4096 keys, 4 key heads
@@ -90,7 +90,8 @@ __device__ __forceinline__ int limit_of(const PagedArgs& a, int len, int fresh, 
 // then holds the keys that the unit's workgroups share; eight units in a row go to the
 // eight XCDs, and the longest sequences come first (of at most 64): the last workgroups to
 // start are short ones.  (Units in order, a run of them an XCD, left the XCD of the longest
-// sequence alone for the last third of the time.)
+// sequence alone for the last third of the time; always in the same direction, the
+// first XCDs had the longer ones of each eight: 8 chunks over up to 4096 keys 144 us for 140.)
 struct Place {
     int split, tile, b, h;
     int64_t unit;
@@ -119,7 +120,7 @@ __device__ __forceinline__ Place place_of(const PagedArgs& a, const Shape& sh, i
         const uint32_t i = block >> 3;
         u = i / per;
         part = i - u * per;
-        u = 8 * u + (block & 7);
+        u = 8 * u + (u & 1 ? 7 - (block & 7) : (block & 7));     // there and back: as much for each XCD
     } else {
         const uint32_t i = block - even * per;
         u = i / per;
