@@ -796,7 +796,11 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
             return;
         }
     } else if (PASS == kSum) {
-        parts_max(sh, row_at, min(tile_rows, rows - first), lane, wave, C::threads / 64, row_max);
+        // a lane a row, the wavefronts share the parts (a wavefront a row took 6 us more)
+        static_assert(PASS != kSum || tile_rows == 64, "a lane is a row");
+        int m = INT_MIN;
+        for (int i = wave; i < sh.splits; i += C::threads / 64) m = max(m, sh.part_max[(row_at + lane) * sh.splits + i]);
+        atomicMax(&row_max[lane], m);
         __syncthreads();
         if (split == 0)
             for (int i = threadIdx.x; i < tile_rows; i += kBlock) sh.row_max[row_at + i] = row_max[i];

@@ -63,10 +63,11 @@ inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int64_t max_keys
         return p;
     }
     // Parts until every compute unit has a workgroup (two, of chunks): of a stage of few rows
-    // (512 keys), of four tiles where they come one by one (256).  Twice the parts of few
-    // rows cost more than they hide (each adds to the results: 131072 keys, 58 us for 49).
+    // (512 keys), of two tiles where they come one by one (24 workgroups of 64 rows over 1001 keys:
+    // 30.7 us, 31.5 with four tiles).  Twice the parts of few rows cost more than they hide (each
+    // adds to the results: 131072 keys, 58 us for 49).
     int64_t want = (p.rows <= 16 ? 256 : 512) / (groups > 0 ? groups : 1);
-    const int64_t most = p.keys / (p.rows <= 16 ? 512 : 256);
+    const int64_t most = p.keys / (p.rows <= 16 ? 512 : 128);
     if (want > most) want = most;
     if (want > 256) want = 256;
     if (want > 1) p.splits = (int32_t)want;
