@@ -33,7 +33,7 @@
 // of 64): 29 us, 3.5 TB/s of the 5.2 that a copy reaches; workgroups of one compute unit
 // read at the same time and then compute at the same time.  One token of a stream of 197 keys:
 // 10 us, a chain of loads and barriers.  One token of 131072 keys (4 key heads of 128): 47 us,
-// three launches of 17, 7 and 21.
+// three launches of 18, 7 and 20.
 //
 // Codes without I-Exp.  e(u), u = max - logit, does not increase with u (the host
 // checks the one place where rounding could make it, the end of an octave), so
@@ -514,6 +514,8 @@ struct Config {
     static constexpr int RG = RG_, KG = KG_;    // row groups, key groups: RG KG wavefronts
     static constexpr int KS = KS_, NV = NV_;    // 64-byte steps and 16-channel tiles of a head
     static constexpr int threads = 64 * RG * KG, rows = 16 * RS * RG;
+    // bytes of LDS: results of the key groups but the first, and 16 rows that a wavefront turns
+    static constexpr int held = (KG - 1) * RG * RS * NV * 1024, turned = 64 * (16 * NV + 4);
 };
 
 // A sum over the lanes of a wavefront: rotations within 16 lanes, then lane swaps.
@@ -964,6 +966,30 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
             for (int ct = 0; ct < NV; ++ct)
                 for (int g = 0; g + 1 < KG; ++g) lo[s][ct] += held[((g * RG + rg) * RS * NV + s * NV + ct) * 64 + lane];
     }
+    if (PASS == kOut) {
+        // Parts add theirs, whole rows at a time: 16 x 4 places 16 bytes apart, as the lanes hold
+        // them, took 3 us more (77 tokens of 3 x 6 heads of 80 in 8 parts).
+        if (stages == 0) return;        // a part without keys
+        int32_t* turn = reinterpret_cast<int32_t*>(dyn) + C::held / 4 + rg * (C::turned / 4);
+        constexpr int ld = 16 * NV + 4;
+#pragma unroll
+        for (int s = 0; s < RS; ++s) {
+            const int row = row0 + 16 * s, n = min(rows - row, 16);
+            const int64_t at = query_of(a, b, h, min(row + (lane & 15), rows - 1)) * a.c.d;
+#pragma unroll
+            for (int ct = 0; ct < NV; ++ct)
+                *reinterpret_cast<i32x4*>(turn + (lane & 15) * ld + 16 * ct + 4 * (lane >> 4)) = lo[s][ct];
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the wavefront's own
+            for (int i = 0; i < n; ++i) {
+                const uint32_t a0 = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, i);
+                const uint32_t a1 = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(at >> 32), i);
+                int32_t* out = a.out + (int64_t)(((uint64_t)a1 << 32) | a0);
+                for (int ch = lane; ch < a.c.d; ch += 64) atomicAdd(out + ch, turn[i * ld + ch]);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        return;
+    }
 #pragma unroll
     for (int s = 0; s < RS; ++s) {
         const int rho = row0 + 16 * s + (lane & 15);
@@ -972,13 +998,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
 #pragma unroll
         for (int ct = 0; ct < NV; ++ct) {
             const int ch = 16 * ct + 4 * (lane >> 4);
-            if (ch >= a.c.d) continue;
-            if (PASS == kOut) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) atomicAdd(out + ch + i, lo[s][ct][i]);
-            } else {
-                *reinterpret_cast<i32x4*>(out + ch) = lo[s][ct];
-            }
+            if (ch < a.c.d) *reinterpret_cast<i32x4*>(out + ch) = lo[s][ct];
         }
     }
 }
@@ -1035,7 +1055,7 @@ void enqueue(const PagedArgs& a, const Shape& sh, const Plan& p, hipStream_t str
     const Mode mode = mode_of(a);
     // the buckets, and after them what the key groups hold
     const size_t buckets = mode != kGeneral ? (size_t)C::rows * sh.buckets * 16 : 0;
-    const size_t held = (size_t)(C::KG - 1) * C::RG * C::RS * C::NV * 1024;
+    const size_t held = C::held + (PASS == kOut ? C::RG * C::turned : 0);
     const size_t logits = KEEP == kLds ? (size_t)(p.rows * p.keys) * 4 : 0;
     const size_t lds = last ? std::max(buckets + logits, held) : 0;
     const bool weight = last && a.c.weight;
