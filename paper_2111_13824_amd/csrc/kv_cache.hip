@@ -175,9 +175,9 @@ __device__ __forceinline__ const int64_t* weight_slot(const CacheView& c, int b,
 // one wavefront takes) from the first bit in which the weights differ; then one scan
 // over the threads places what is heavier and as many of its equals, from the lowest
 // place on, as are missing.  (A histogram that one thread walks takes 10 us a digit.)
-// Bound by the digits' passes, some 2 us each: 128 units of up to 8192 weights, 5 MB, 12.8 us;
-// 14.5 with one histogram, whose first bins' additions, weights of all sizes in them,
-// wait for each other.
+// Bound by latency, of three loads in a row and of the digits' passes: 128 units of up to 8192
+// weights, 5 MB, 11.8 us (12.3 where all digits are looked at, 14.5 with one histogram, whose
+// first bins' additions, weights of all sizes in them, wait for each other).
 template <int ITEMS>
 __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
     __shared__ uint32_t hist[kCopies][257];     // copies begin in different banks
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
     const int top = diff ? 64 - __clzll((long long)diff) : 0;
     uint64_t prefix = top < 64 ? w0 >> top << top : 0;
     int need = m;
-    for (int hi = top; hi > 0;) {
+    for (int hi = top; hi > 0 && need > 0;) {
         const int lo = max(hi - 8, 0);
         const uint32_t mask = (1u << (hi - lo)) - 1;
         for (int i = tid; i < kCopies * 257; i += kSelect) (&hist[0][0])[i] = 0;
@@ -267,8 +267,12 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if ((uint32_t)need > before && (uint32_t)need <= before + v[e]) {
-                    bound = prefix | ((uint64_t)(255 - 4 * lane - e) << lo);
-                    missing = need - (int)before;
+                    const uint64_t at = prefix | ((uint64_t)(255 - 4 * lane - e) << lo);
+                    const int left = need - (int)before;
+                    // all of this bin stay: what is heavier than the weight below it
+                    const bool all = (uint32_t)left == v[e] && at != 0;
+                    bound = all ? at - 1 : at;
+                    missing = all ? 0 : left;
                 }
                 before += v[e];
             }

@@ -32,7 +32,7 @@
 // workgroups end before the longest).  One token of 64 streams (4096 keys, 4 key heads
 // of 64): 29 us, 3.5 TB/s of the 5.2 that a copy reaches; workgroups of one compute unit
 // read at the same time and then compute at the same time.  One token of a stream of 197 keys:
-// 10 us, a chain of loads and barriers.  One token of 131072 keys (4 key heads of 128): 47 us,
+// 10 us, a chain of loads and barriers.  One token of 131072 keys (4 key heads of 128): 45 us,
 // three launches of 18, 7 and 20.
 //
 // Codes without I-Exp.  e(u), u = max - logit, does not increase with u (the host
