@@ -180,6 +180,15 @@ ATTEND = [
     (1, 16, 1, 1, 64, 128, [3000], [1], dict(s=2e-4, n=14, zp_q=-128, zp_v=5)),
     (3, 8, 1, 2, 128, 64, [2049, 0, 1500], [2, 2, 0], dict(causal=False)),
     (65, 2, 1, 2, 16, 16, [3 * i % 50 for i in range(65)], [2] * 65, {}),
+    # narrow heads in parts, the 64-bit form in parts, parts that only some sequences fill
+    (2, 4, 2, 24, 32, 16, [2500, 1100], [24, 20], dict(zp_q=3, zp_v=-4)),
+    (1, 6, 2, 30, 16, 32, [1700], [30], dict(causal=False, bits=2)),
+    (1, 4, 1, 17, 80, 64, [1800], [17], dict(s=0.1, n=30)),
+    (3, 4, 2, 50, 48, 256, [3000, 200, 60], [50, 50, 40], {}),
+    # chunks of so many heads that their keys stay whole: more than 16 tiles of 64 keys, in
+    # pages that hold a tile and in smaller ones
+    (16, 32, 32, 17, 16, 64, [2300 - 120 * i for i in range(16)], [17 - i % 3 for i in range(16)], {}),
+    (8, 64, 64, 17, 16, 16, [1090, 1025, 1024, 1500, 2049, 17, 0, 1], [17] * 8, dict(zp_q=2)),
 ]
 
 
