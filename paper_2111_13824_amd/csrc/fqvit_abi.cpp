@@ -563,7 +563,7 @@ fq_status rmsnorm(const int8_t* x, int32_t zp_x, const uint8_t* alpha, int32_t K
     a.x = x;
     a.alpha = x ? alpha : nullptr;
     a.zp_x = zp_x;
-    a.K = K;
+    a.K = a.alpha ? K : 0;      // factors of 0 are not clamped below 0 by a K that is not looked at
     a.m_x = m_x;
     a.r = r;
     a.gamma = gamma;

@@ -33,4 +33,6 @@ void fq_test_integers(long long* out) {
     out[1] = fqvit::g_paged.c.log2_page;
     out[2] = fqvit::g_rms.alpha != nullptr;
 }
+// the bound of the last norm's factors
+int fq_test_norm_bound(void) { return fqvit::g_rms.K; }
 }
