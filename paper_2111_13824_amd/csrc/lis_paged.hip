@@ -462,6 +462,12 @@ struct RowAdder {
     }
 };
 
+// The middle one of three integers, in a form that the compiler takes as one instruction.  (Not
+// inline asm: it would not wait for a matrix instruction that is still writing x.)
+__device__ __forceinline__ int median(int x, int lo, int hi) {
+    return max(min(x, lo), min(max(x, lo), hi));
+}
+
 // Bytes 0..3 of the result: byte 3 of each word.
 __device__ __forceinline__ uint32_t top_bytes(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
     return __builtin_amdgcn_perm(x1, x0, 0x0c0c0703u) | __builtin_amdgcn_perm(x3, x2, 0x07030c0cu);
@@ -890,8 +896,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (FAST) {
-                        int u;          // U_1 - 1 - u
-                        asm("v_med3_i32 %0, %1, %2, 0" : "=v"(u) : "v"(acc[s][t][i]), "s"(-cap));
+                        const int u = median(acc[s][t][i], -cap, 0);    // U_1 - 1 - u
                         x[i] = end[(u >> sh.shift) * 64] + (uint32_t)u;
                     } else {
                         uint32_t z;
