@@ -940,9 +940,10 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
             const uint32_t sum = sum16(got, lane);          // of key lane % 16 of the lane's block
             const int at = min(key0 + 16 * (lane >> 4), (len - 1) & ~15);
             const int id = a.c.table[(int64_t)b * a.c.max_pages + (at >> a.c.log2_page)];
-            const int64_t slot = (((int64_t)((uint32_t)id < (uint32_t)a.c.pages ? id : 0) * a.c.Hkv + h) << a.c.log2_page) +
-                                 (at & ((1 << a.c.log2_page) - 1));
-            if (sum) atomicAdd(reinterpret_cast<unsigned long long*>(a.c.weight) + slot + (lane & 15), (unsigned long long)sum);
+            // an id that is no page is not written through
+            const int64_t slot = (((int64_t)id * a.c.Hkv + h) << a.c.log2_page) + (at & ((1 << a.c.log2_page) - 1));
+            if (sum && (uint32_t)id < (uint32_t)a.c.pages)
+                atomicAdd(reinterpret_cast<unsigned long long*>(a.c.weight) + slot + (lane & 15), (unsigned long long)sum);
         }
     };
 #pragma unroll
