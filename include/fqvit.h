@@ -524,9 +524,10 @@ fq_status rmsnorm_rows_int8(const int8_t* x, int32_t zp_x, const uint8_t* alpha,
  *   length   [B] int32: keys of each sequence, in [0, max_pages page].
  * pages in [1, 2^30], page a power of two in [16, 1024], d a multiple of 16 in
  * [16, 128], max_pages page at most 2^20, Hkv in [1, 1024], B Hkv in [0, 65536].
- * table and length are device arrays and cannot be checked here: a length is taken
- * within [0, max_pages page]; a table entry that names no page reads as page 0 and is
- * never written through.  Sequences may share pages that no call writes.
+ * table and length are device arrays and cannot be checked here: of a longer length the
+ * keys are those that the table can name, and new tokens (the last of it) may have places
+ * beyond them; a length below 0 is 0.  A table entry that names no page reads as page 0 and
+ * is never written through.  Sequences may share pages that no call writes.
  */
 
 /*
@@ -557,7 +558,8 @@ fq_status kv_cache_append_int8(const int8_t* k, const int8_t* v, int32_t B, int3
  *           hq reads key head hq / r.  L in [0, 2^20], L r below 2^30.
  *   n_new   NULL (L) or [B] int32 in [0, L]: token i < n_new[b] stands at place
  *           length[b] - n_new[b] + i.  Rows behind n_new[b] are neither read nor written.
- *   causal  1: a token sees the places up to its own; 0: all keys of its sequence.
+ *   causal  1: a token sees the keys up to its own place (all where that is beyond the
+ *           table, none where it is negative); 0: all keys of its sequence.
  *   zp_k    does not change the result (see lis_attention_qk); it is validated.
  *   s_logit, bits (in [1, 4]), exp_n: as in lis_attention_head.
  *   out     [B, Hq, L, d] int32, 16-byte aligned: for a token that sees the keys J,

@@ -13,6 +13,13 @@ __device__ __forceinline__ int keys_of(const CacheView& c, int b) {
     return min(max(c.length[b], 0), c.max_pages << c.log2_page);
 }
 
+// Place of the first of n (<= 2^20) new tokens of sequence b, its last keys: below 0 or beyond
+// the table where the length says so.  No key lies beyond 2^20, so a length of 2^30 stands for
+// all above it, and 0 for all below.
+__device__ __forceinline__ int first_new(const CacheView& c, int b, int n) {
+    return min(max(c.length[b], 0), 1 << 30) - n;
+}
+
 // The page at place `at` (< max_pages) of sequence b's table.  An id that is no
 // page of the cache reads as page 0: never a place outside the cache.
 __device__ __forceinline__ int page_at(const int32_t* table, int max_pages, int pages, int b, int at) {

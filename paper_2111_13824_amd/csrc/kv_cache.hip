@@ -33,7 +33,7 @@ struct NewKeys {
 // Tokens whose place would lie before the first or beyond the table are left out.
 __device__ __forceinline__ NewKeys new_keys(const AppendArgs& a, int b) {
     const int n = a.n_new ? min(max(a.n_new[b], 0), a.L) : a.L;
-    return NewKeys{a.c.length[b] - n, n};
+    return NewKeys{cache::first_new(a.c, b, n), n};
 }
 
 __device__ __forceinline__ bool in_table(const CacheView& c, int place) {

@@ -59,6 +59,7 @@
 namespace fqvit {
 namespace {
 
+using cache::first_new;
 using cache::head_base;
 using cache::keys_of;
 using cache::page_at;
@@ -82,8 +83,9 @@ __device__ __forceinline__ int64_t query_of(const PagedArgs& a, int b, int h, in
     return ((int64_t)b * a.Hq + h * a.group + g) * a.L + i;
 }
 
-__device__ __forceinline__ int limit_of(const PagedArgs& a, int len, int fresh, int rho) {
-    return a.causal ? min(max(len - fresh + rho / a.group + 1, 0), len) : len;
+// Keys that row rho sees, of `len`; `past`: the place of the first new token.
+__device__ __forceinline__ int limit_of(const PagedArgs& a, int len, int past, int rho) {
+    return a.causal ? min(max(past + rho / a.group + 1, 0), len) : len;
 }
 
 // What a workgroup works on.  Its unit, a sequence's key head, runs on one XCD, whose L2
@@ -567,13 +569,13 @@ __device__ __forceinline__ uint64_t sum4(i32x4 v, int key0, int end, int mx, con
 // another, every lane four keys of each; rows fewer than the wavefronts are shared by
 // them.  done(row, sum): of what the wavefront took.  logits(row): the row's.
 template <bool FAST, typename L, typename F>
-__device__ __forceinline__ void sum_rows(const PagedArgs& a, int len, int fresh, int rows, int from, int to,
+__device__ __forceinline__ void sum_rows(const PagedArgs& a, int len, int past, int rows, int from, int to,
                                          int lane, int wave, int waves, const int* row_max, L&& logits, F&& done) {
     const int share = rows < waves ? waves / rows : 1;          // wavefronts a row
     const int first = share > 1 ? wave % rows : wave, part = share > 1 ? wave / rows : 0;
     if (part >= share) return;
     for (int row = first; row < rows; row += waves) {
-        const int end = min(to, limit_of(a, len, fresh, row)), mx = row_max[row];
+        const int end = min(to, limit_of(a, len, past, row)), mx = row_max[row];
         const auto* p = logits(row);
         uint64_t sum = 0;
         for (int key = from + 256 * part + 4 * lane; key < end; key += 256 * share)
@@ -615,7 +617,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     const int64_t unit = at.unit;
     const int len = keys_of(a.c, b);
     const int fresh = a.n_new ? min(max(a.n_new[b], 0), a.L) : a.L;
-    const int rows = fresh * a.group;
+    const int rows = fresh * a.group, past = first_new(a.c, b, fresh);
     const int first = tile * tile_rows;             // the workgroup's first row
     if (first >= rows) return;
     const int row0 = first + rg * kRows;            // the wavefront's
@@ -623,13 +625,13 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
 
     int limit[RS];
 #pragma unroll
-    for (int s = 0; s < RS; ++s) limit[s] = limit_of(a, len, fresh, min(row0 + 16 * s + (lane & 15), rows - 1));
+    for (int s = 0; s < RS; ++s) limit[s] = limit_of(a, len, past, min(row0 + 16 * s + (lane & 15), rows - 1));
     // keys that every row of the wavefront sees, and that some row of the workgroup does
-    const int full = limit_of(a, len, fresh, min(row0, rows - 1));
-    const int all = limit_of(a, len, fresh, min(first + tile_rows, rows) - 1);
+    const int full = limit_of(a, len, past, min(row0, rows - 1));
+    const int all = limit_of(a, len, past, min(first + tile_rows, rows) - 1);
     const int per = ((all + kTile - 1) / kTile + sh.splits - 1) / sh.splits * kTile;
     const int from = min(split * per, all), until = min(from + per, all);
-    const int to = idle ? 0 : min(until, limit_of(a, len, fresh, min(row0 + kRows, rows) - 1));
+    const int to = idle ? 0 : min(until, limit_of(a, len, past, min(row0 + kRows, rows) - 1));
     const int whole = min(full, to);                // tiles that end here or before are seen whole
     const int stages = (until - from + KG * kTile - 1) / (KG * kTile);
 
@@ -827,7 +829,7 @@ __global__ __launch_bounds__(C::threads, 2) void lis_paged_kernel(PagedArgs a, S
     if (PASS == kAll || PASS == kSum) {
         if (KEEP == kLds) {
             prime(No{}, Yes{});
-            sum_rows<FAST>(a, len, fresh, rows, from, until, lane, wave, KG * RG, row_max,
+            sum_rows<FAST>(a, len, past, rows, from, until, lane, wave, KG * RG, row_max,
                            [&](int row) { return lds_logits + row * (int)sh.keys; },
                            [&](int row, uint64_t v) { atomicAdd(&row_sum[row], (unsigned long long)v); });
         } else {
@@ -1021,9 +1023,9 @@ __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shap
     const int64_t unit = place.unit;
     const int len = keys_of(a.c, b);
     const int fresh = a.n_new ? min(max(a.n_new[b], 0), a.L) : a.L;
-    const int rows = fresh * a.group;
+    const int rows = fresh * a.group, past = first_new(a.c, b, fresh);
     if (rows == 0) return;
-    const int all = limit_of(a, len, fresh, rows - 1);
+    const int all = limit_of(a, len, past, rows - 1);
     const int per = ((all + kTile - 1) / kTile + sh.splits - 1) / sh.splits * kTile;
     const int from = min(split * per, all), to = min(from + per, all);
     const int64_t row_at = unit * 16;
@@ -1032,7 +1034,7 @@ __global__ __launch_bounds__(kBlock) void lis_paged_sum_kernel(PagedArgs a, Shap
     __syncthreads();
     if (split == 0 && threadIdx.x < rows) sh.row_max[row_at + threadIdx.x] = row_max[threadIdx.x];
     const int32_t* lg = sh.logits + unit * sh.rows * sh.keys;
-    sum_rows<FAST>(a, len, fresh, rows, from, to, lane, wave, kBlock / 64, row_max,
+    sum_rows<FAST>(a, len, past, rows, from, to, lane, wave, kBlock / 64, row_max,
                    [&](int row) { return lg + row * sh.keys; },
                    [&](int row, uint64_t v) { atomicAdd(&row_sum[row], (unsigned long long)v); });
     __syncthreads();
