@@ -570,7 +570,9 @@ fq_status kv_cache_append_int8(const int8_t* k, const int8_t* v, int32_t B, int3
  *           (64-bit integer atomics: the sums do not depend on their order.)
  *   workspace  device scratch of fq_lis_attention_paged_workspace_bytes(B, Hq, Hkv, L,
  *           d, max_pages * page) bytes, 16-byte aligned, of one call at a time (NULL where that
- *           is 0); its contents on entry do not matter.
+ *           is 0); its contents on entry do not matter.  It grows with what the table can
+ *           name, not with the lengths: for at most 16 rows (L r) of a key head 4 bytes for each
+ *           row and key while that is at most 1 GiB in all, and never more than 17 MB beside.
  * Every row's sum is exact in 64 bits and out in 32: |out| <= 255 (1.5 2^15 + 2^20).
  * Errors: FQ_ERR_NULL, FQ_ERR_SHAPE (sizes, Hq, or 2^24 or more workgroups), FQ_ERR_PARAM
  * (zero points, causal, bits, exp_n, s_logit, alignment, workspace too small),

@@ -1120,16 +1120,7 @@ size_t lis_paged_workspace(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int32_
 
 hipError_t launch_lis_paged(const PagedArgs& a, hipStream_t stream) {
     const Plan p = paged::plan(a.c.B, a.Hq, a.c.Hkv, a.L, (int64_t)a.c.max_pages << a.c.log2_page);
-    Shape sh{};
-    sh.splits = p.splits;
-    sh.tiles = p.tiles;
-    sh.rows = p.rows;
-    sh.keys = p.keys;
-    // the sums first: they need the largest alignment
-    sh.row_sum = static_cast<uint64_t*>(a.workspace);
-    sh.row_max = reinterpret_cast<int32_t*>(sh.row_sum + p.all_rows());
-    sh.part_max = sh.row_max + p.all_rows();
-    sh.logits = sh.part_max + p.all_rows() * p.splits;
+    Shape sh = paged::shape(p, a.workspace);
     while ((2u << sh.shift) <= a.k.d_ln2) ++sh.shift;       // 2^shift <= q_ln2
     const int cap = (a.k.n < a.k.top ? a.k.n : a.k.top) * (int)a.k.d_ln2 + 1;
     sh.buckets = ((cap - 1) >> sh.shift) + 2;

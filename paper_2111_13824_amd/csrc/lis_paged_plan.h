@@ -19,6 +19,15 @@ enum Way { kOne, kOneFew, kParts, kPartsFew };
 // Logits of a workgroup that LDS holds beside two stages, the buckets and the rest.
 constexpr int64_t kLdsLogits = 16384;
 
+// Logits that the workspace holds: 1 GiB.  They are as many as the table can name, whatever the
+// lengths are (which are on the device), and tables of 2^20 keys for 128 key heads of 16 rows
+// would take 8 GiB.  Calls beyond it take the logits again, as those of more rows do, which
+// costs most with few rows and long sequences: tables of 131072 keys for 512 key heads of 64
+// channels, stored to again, 4 rows (1 GiB) 26 us to 25, 79 to 99 and 313 to 405 of 512, 4096 and
+// 16384 keys, 8 rows (2 GiB) 31 to 25, 109 to 100 and 440 to 405; heads of 128, 8 rows, 39 to 32,
+// 166 to 175 and 608 to 717.
+constexpr int64_t kMostLogits = (int64_t)1 << 28;
+
 struct Plan {
     Way way;
     int32_t splits;         // parts of the keys, each a workgroup's
@@ -62,19 +71,36 @@ inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int64_t max_keys
         p.way = kOneFew;
         return p;
     }
+    const bool few = p.rows <= 16 && p.units * p.rows * p.keys <= kMostLogits;
+    if (!few) p.tile_rows = 64;         // (one tile of at most 16 rows stays one)
     // Parts until every compute unit has a workgroup (two, of chunks): of a stage of few rows
     // (512 keys), of two tiles where they come one by one (24 workgroups of 64 rows over 1001 keys:
     // 30.7 us, 31.5 with four tiles).  Twice the parts of few rows cost more than they hide (each
     // adds to the results: 131072 keys, 58 us for 49).
-    int64_t want = (p.rows <= 16 ? 256 : 512) / (groups > 0 ? groups : 1);
-    const int64_t most = p.keys / (p.rows <= 16 ? 512 : 128);
+    int64_t want = (few ? 256 : 512) / (groups > 0 ? groups : 1);
+    const int64_t most = p.keys / (few ? 512 : 128);
     if (want > most) want = most;
     if (want > 256) want = 256;
     if (want > 1) p.splits = (int32_t)want;
     // three launches cost what four tiles in a row do: chunks of few keys stay in one
-    if (p.rows > 16 && p.keys < 1024) p.splits = 1;
-    p.way = p.rows <= 16 ? kPartsFew : (p.splits > 1 ? kParts : kOne);
+    if (!few && p.keys < 1024) p.splits = 1;
+    p.way = few ? kPartsFew : (p.splits > 1 ? kParts : kOne);
     return p;
+}
+
+// The plan's arrays in a workspace of its bytes(); the sums first, which need the largest
+// alignment.
+inline Shape shape(const Plan& p, void* workspace) {
+    Shape sh{};
+    sh.splits = p.splits;
+    sh.tiles = p.tiles;
+    sh.rows = p.rows;
+    sh.keys = p.keys;
+    sh.row_sum = static_cast<uint64_t*>(workspace);
+    sh.row_max = reinterpret_cast<int32_t*>(sh.row_sum + p.all_rows());
+    sh.part_max = sh.row_max + p.all_rows();
+    sh.logits = sh.part_max + p.all_rows() * p.splits;
+    return sh;
 }
 
 }  // namespace paged
