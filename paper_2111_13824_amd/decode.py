@@ -145,12 +145,13 @@ def kv_cache_append_int8(k, v, k_pages, v_pages, table, length, n_new=None, weig
 def lis_attention_paged_workspace_bytes(B: int, Hq: int, Hkv: int, L: int, d: int,
                                         max_keys: int) -> int:
     """Bytes of device scratch that lis_attention_paged needs (max_keys: keys that a
-    table's row can name); 0 where it needs none, and for invalid sizes."""
+    table's row can name, which it grows with, to 1 GiB); 0 where it needs none, and
+    for invalid sizes."""
     return _workspace_bytes(B, Hq, Hkv, L, d, max_keys)
 
 
 def _workspace_bytes(*sizes) -> int:
-    if max(sizes[:5]) > 0x7fffffff or min(sizes) < 0:       # the call itself refuses these
+    if max(sizes) > 0x7fffffff or min(sizes) < 0:       # the call itself refuses these
         return 0
     return (_b._lib or _b.lib()).fq_lis_attention_paged_workspace_bytes(*sizes)
 
