@@ -336,8 +336,11 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
 // so, by the workgroups z = 0; in other pages the order does not matter.  A workgroup
 // moves the keys (x = 0), 16 channels of the values, or the weights (the last x) of one
 // sequence and head.  Bound by memory: of a quarter of the keys nearly all lines of the
-// values come in (128 units, 2048 of up to 8192 keys of 64: about 100 MB in 21 us;
-// writing four keys as one word changed nothing).
+// values come in (128 units, 2048 of up to 8192 keys of 64: 69 MB read and 34 written in
+// 31 us, a copy of as much would take 20; writing four keys as one word changed nothing).
+// In place one workgroup a part walks the tiles one after another, and a key that stays where it
+// is is written again: 16 such sequences take 15 us more, one sequence of 131072 keys cut to
+// 32768 307 us in all, in other pages 33.
 constexpr int kMoveUnits = 8;       // 16-byte units a thread holds
 
 __global__ __launch_bounds__(kBlock) void evict_move_kernel(EvictArgs a) {

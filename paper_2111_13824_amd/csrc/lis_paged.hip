@@ -24,12 +24,13 @@
 // The row's maximum is needed before the first I-Exp, its exact sum before the first
 // code: three passes over the keys.  The matrix cores are far from busy (a logit costs
 // them less than one vector instruction), so each pass takes the logits again; a call
-// of at most 16 rows a key head, which the keys' bytes bound, stores them instead.
+// of at most 16 rows a key head, which the keys' bytes bound, stores them instead where
+// they fit.
 //
-// Measured.  Chunks (8 of up to 512 tokens and 16 heads of 64, 4096 keys): 140 us, 36 GOP;
-// bound by vector instructions, 41 million for the codes and sums, a compute unit busy 70 % of
-// the time (maximum 18 us, sum 44, codes and product 38, and the shorter sequences'
-// workgroups end before the longest).  One token of 64 streams (4096 keys, 4 key heads
+// Measured.  Chunks (8 of up to 512 tokens and 16 heads of 64, 4096 keys): 139 to 158 us by
+// their lengths, 36 GOP; bound by vector instructions, 45 million, which are 73 us of issue:
+// about half of the time, as the shorter sequences' workgroups end before the
+// longest.  One token of 64 streams (4096 keys, 4 key heads
 // of 64): 29 us, 3.5 TB/s of the 5.2 that a copy reaches; workgroups of one compute unit
 // read at the same time and then compute at the same time.  One token of a stream of 197 keys:
 // 10 us, a chain of loads and barriers.  One token of 131072 keys (4 key heads of 128): 45 us,

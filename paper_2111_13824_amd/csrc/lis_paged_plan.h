@@ -23,9 +23,9 @@ constexpr int64_t kLdsLogits = 16384;
 // lengths are (which are on the device), and tables of 2^20 keys for 128 key heads of 16 rows
 // would take 8 GiB.  Calls beyond it take the logits again, as those of more rows do, which
 // costs most with few rows and long sequences: tables of 131072 keys for 512 key heads of 64
-// channels, stored to again, 4 rows (1 GiB) 26 us to 25, 79 to 99 and 313 to 405 of 512, 4096 and
-// 16384 keys, 8 rows (2 GiB) 31 to 25, 109 to 100 and 440 to 405; heads of 128, 8 rows, 39 to 32,
-// 166 to 175 and 608 to 717.
+// channels, stored to again, a row (256 MiB) 24 us to 25, 64 to 99 and 236 to 404 of 512, 4096 and
+// 16384 keys, 4 rows (1 GiB) 26 to 25, 79 to 99 and 313 to 405, 8 rows (2 GiB) 31 to 25, 109 to
+// 100 and 440 to 405; heads of 128, 8 rows, 39 to 32, 166 to 175 and 608 to 717.
 constexpr int64_t kMostLogits = (int64_t)1 << 28;
 
 struct Plan {
@@ -65,8 +65,9 @@ inline Plan plan(int32_t B, int32_t Hq, int32_t Hkv, int32_t L, int64_t max_keys
     p.tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
     const int64_t groups = p.units * p.tiles;
     // One launch of a workgroup a unit takes 4 us and 2 more for every 512 keys, three launches
-    // 18 to some thousands of keys; with workgroups for half the compute units they are even
-    // (4 units of 1024, 2048 and 4096 keys: 12, 16 and 24 us to 18).
+    // 18 to some thousands of keys: of few units, 1024, 2048 and 4096 keys 12, 16 and 24 us to 18.
+    // With workgroups for half the compute units it is one launch as far as LDS goes: 4096 keys of
+    // 128 units of a row 22 us to 28, of 256 of a row 27 to 37, of 256 of 4 rows 29 to 46.
     if (p.rows <= 16 && p.rows * p.keys <= kLdsLogits && (p.keys <= 2048 || p.units >= 128)) {
         p.way = kOneFew;
         return p;
